@@ -54,7 +54,8 @@ enum {
 };
 
 typedef enum { DLF_CONV = 0, DLF_DWCONV = 1, DLF_FC = 2, DLF_MAXPOOL = 3, DLF_GAVGPOOL = 4 } dlf_op;
-typedef enum { DLF_ACT_NONE = 0, DLF_ACT_RELU = 1, DLF_ACT_RELU6 = 2 } dlf_act;
+/* (a layer list's layers take the first three) */
+typedef enum { DLF_ACT_NONE = 0, DLF_ACT_RELU = 1, DLF_ACT_RELU6 = 2, DLF_ACT_GELU = 3, DLF_ACT_GELU_TANH = 4, DLF_ACT_SILU = 5 } dlf_act;
 
 /* One layer, in the paper's {C_in, C_out, H_out x W_out, K_h x K_w} notation (Sec. II-B) plus
  * what the fused epilogue needs.  BatchNorm is folded into the bias. */
@@ -284,6 +285,84 @@ int dlf_net_set_option(dlf_net* net, int option, int value);
 int dlf_conv_chain_run_static(const dlf_layer_desc* layers, int n_layers, int N, int H, int W,
                               const void* x_f16_dev, const void* const* w_f16_dev,
                               const float* const* bias_dev, void* y_f16_dev, int sm_count, void* stream);
+
+/* ---- dense operators: fully connected layers and gated blocks, forwards and backwards ------------------------------------
+ * (The paper has no counterpart for these calls.)
+ *
+ * Standalone operators beside the layer list, for models whose dense parts are trained, run in bf16, or see another number of
+ * rows ("tokens") at every call.  Matrices are row-major and 16 bits wide, all of a call of one dlf_dtype; ld* is the number of
+ * elements from one row's start to the next (at least the columns; any value where there is one row).  Weights are [n][k], one row per output.  Biases and their gradients
+ * are fp32 vectors of n.  Products are summed in fp32 and every result is rounded to nearest even once.
+ *
+ *   dlf_linear        z = x w^T + bias + res,  y = act(z)          x [m][k], w [n][k], res, y, z [m][n]
+ *   dlf_linear_grad   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum over the rows of dz   (dz is also res's gradient)
+ *   dlf_gated         g = x wg^T + bg,  u = x wu^T + bu,  h = act(g) u          x [m][k], wg, wu [n][k], h, g, u [m][n]
+ *   dlf_gated_grad    dg = dh u act'(g),  du = dh act(g),  dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x,  dbg, dbu
+ *
+ * act: RELU (0 for a NaN, as everywhere here), RELU6, GELU (v Phi(v)), GELU_TANH (its form with tanh), SILU (v / (1 + e^-v)).
+ * Their derivatives are taken at z and g as the forward call stored them; at a corner of RELU and RELU6 the derivative is 0.
+ * dz, dg and du are rounded to 16 bits, once, before they enter the products (db, dbg and dbu sum the values before that).
+ *
+ * Optional (null): bias, res, z, bg, bu, g, u of the forward calls; every output of the backward calls, and the inputs that
+ * none of the outputs asked for needs (z without an activation, w without dx, x without dw, and so on).  y may be res itself
+ * (same pointer and ld), dz may be dy or z; else no output may overlap an input or another output.
+ * m may be 0 (weights' and biases' gradients are then 0); n and k are at least 1; no size exceeds 2^30.
+ * Pointers need the alignment of their element only.  Rows that start on 16-byte boundaries (pointer 16-byte aligned, ld a
+ * multiple of 8) are fastest.
+ *
+ * A call enqueues on `stream` of the current device and returns; it allocates nothing, keeps nothing between calls, may be
+ * captured into a graph, and may run beside others on other streams.  workspace_dev: 256-byte aligned, at least as large as
+ * dlf_*_workspace_bytes says for the same arguments (that call looks at sizes, ld and alignment, and at which pointers are null;
+ * 0: none needed, null will do); its contents are the call's from its launch to its completion.  Errors: DLF_E_INVALID_ARG, DLF_E_SHAPE,
+ * DLF_E_WORKSPACE, DLF_E_CUDA; nothing is enqueued then (except by a launch that fails with DLF_E_CUDA behind others).  The same call gives the same bits. */
+typedef enum { DLF_F16 = 0, DLF_BF16 = 1 } dlf_dtype;
+
+typedef struct {
+    int32_t dtype, act;
+    int64_t m, k, n;
+    const void *x, *w;
+    const float* bias;
+    const void* res;
+    void *y, *z;
+    int64_t ldx, ldw, ldres, ldy, ldz;
+} dlf_linear_args;
+
+typedef struct {
+    int32_t dtype, act;
+    int64_t m, k, n;
+    const void *dy, *x, *w, *z;
+    void *dx, *dw;
+    float* db;
+    void* dz;
+    int64_t lddy, ldx, ldw, ldz, lddx, lddw, lddz;
+} dlf_linear_grad_args;
+
+typedef struct {
+    int32_t dtype, act;
+    int64_t m, k, n;
+    const void *x, *wg, *wu;
+    const float *bg, *bu;
+    void *h, *g, *u;
+    int64_t ldx, ldwg, ldwu, ldh, ldg, ldu;
+} dlf_gated_args;
+
+typedef struct {
+    int32_t dtype, act;
+    int64_t m, k, n;
+    const void *dh, *x, *wg, *wu, *g, *u;
+    void *dx, *dwg, *dwu;
+    float *dbg, *dbu;
+    int64_t lddh, ldx, ldwg, ldwu, ldg, ldu, lddx, lddwg, lddwu;
+} dlf_gated_grad_args;
+
+int dlf_linear_workspace_bytes(const dlf_linear_args* args, size_t* bytes);
+int dlf_linear(const dlf_linear_args* args, void* workspace_dev, size_t bytes, void* stream);
+int dlf_linear_grad_workspace_bytes(const dlf_linear_grad_args* args, size_t* bytes);
+int dlf_linear_grad(const dlf_linear_grad_args* args, void* workspace_dev, size_t bytes, void* stream);
+int dlf_gated_workspace_bytes(const dlf_gated_args* args, size_t* bytes);
+int dlf_gated(const dlf_gated_args* args, void* workspace_dev, size_t bytes, void* stream);
+int dlf_gated_grad_workspace_bytes(const dlf_gated_grad_args* args, size_t* bytes);
+int dlf_gated_grad(const dlf_gated_grad_args* args, void* workspace_dev, size_t bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -14,6 +14,8 @@ OK, E_INVALID_ARG, E_SHAPE, E_PLAN, E_WORKSPACE, E_UNSUPPORTED, E_CUDA, E_TIMEOU
     0, -1, -2, -3, -4, -5, -6, -7, -8)
 OPS = {"conv": 0, "dwconv": 1, "fc": 2, "maxpool": 3, "gavgpool": 4}
 ACTS = {"none": 0, "relu": 1, "relu6": 2}
+DENSE_ACTS = {**ACTS, "gelu": 3, "gelu_tanh": 4, "silu": 5}   # of the dense operators
+DTYPES = {"f16": 0, "bf16": 1}
 OPT_NO_TENSOR_CORE, OPT_SINGLE_AS_CHAIN, OPT_CUDA_GRAPH, OPT_PDL, OPT_CONV_ROW_MODE, OPT_GROUP_KERNEL = 1, 3, 4, 5, 6, 7
 
 
@@ -82,6 +84,9 @@ def lib():
             "dlf_conv_chain_run_static": (C.c_int, [C.POINTER(LayerDesc), C.c_int, C.c_int, C.c_int, C.c_int, vp,
                                                     C.POINTER(vp), C.POINTER(vp), vp, C.c_int, vp]),
         }
+        for op in ("dlf_linear", "dlf_linear_grad", "dlf_gated", "dlf_gated_grad"):   # (their arguments: a packed struct)
+            sig[op] = (C.c_int, [C.c_char_p, vp, C.c_size_t, vp])
+            sig[op + "_workspace_bytes"] = (C.c_int, [C.c_char_p, C.POINTER(C.c_size_t)])
         for name, (res, args) in sig.items():
             f = getattr(L, name)
             f.restype, f.argtypes = res, args

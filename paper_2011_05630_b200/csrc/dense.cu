@@ -1,0 +1,378 @@
+// Host side of the dense operators (dlf_linear*, dlf_gated*), and the pass that takes gradients back through an activation.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "dense.h"
+#include "dense_math.cuh"
+#include "ptx.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace dlf {
+
+namespace {
+
+// ---- gradients behind an activation ----------------------------------------------------------------------------------------
+// Bound by memory: 2 or 3 matrices are read, 1 or 2 written, once each.  A CTA owns 64 columns (128 bytes of a row: whole lines)
+// and walks rows, so that a column's sum stays in one thread's registers; kGradSplit CTAs share the rows of a strip as a cluster
+// and their column sums meet in distributed shared memory, added up in the order of the ranks: the same bits every time, no
+// atomics and no second kernel.
+constexpr int kGradCols = 64, kGradThreads = 256, kGradSplit = 8;
+
+template <typename T, int V>
+__device__ __forceinline__ void load_run(const Mat& m, int64_t row, int64_t col, int n, float (&v)[V]) {
+    const T* p = static_cast<const T*>(m.p) + row * m.ld + col;
+    if (V == 8 && n == 8) {
+        const uint4 q = ld_map(reinterpret_cast<const uint4*>(p));
+        const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = to_f32(e[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = i < n ? to_f32(ld_map(p + i)) : 0.0f;
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_run(const Mat& m, int64_t row, int64_t col, int n, const float (&v)[V]) {
+    if (!m.p) return;
+    T* p = static_cast<T*>(const_cast<void*>(m.p)) + row * m.ld + col;
+    if (V == 8 && n == 8) {
+        uint4 q;
+        T* e = reinterpret_cast<T*>(&q);
+#pragma unroll
+        for (int i = 0; i < V; i++) e[i] = from_f32<T>(v[i]);
+        *reinterpret_cast<uint4*>(p) = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++)
+            if (i < n) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+template <typename T, int V, bool GATED>
+__global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThreads) dense_grad_kernel(const __grid_constant__ DenseGrad g) {
+    constexpr int TX = kGradCols / V, TY = kGradThreads / TX;
+    __shared__ float red[GATED ? 2 : 1][TY][kGradCols];
+    pdl_wait();
+    pdl_launch_dependents();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = static_cast<int>(cluster.block_rank());
+    const int64_t strip = blockIdx.x / kGradSplit;
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
+    const int64_t col = strip * kGradCols + tx * V;
+    const int n = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(V), g.N - col)));
+    float s0[V] = {}, s1[V] = {};
+    if (n > 0)
+        with_act(g.act, [&](auto act) {
+            // (rows are dealt out round by round, so that the CTAs of a strip are never more than TY rows of work apart)
+#pragma unroll 2
+            for (int64_t row = static_cast<int64_t>(rank) * TY + ty; row < g.M; row += static_cast<int64_t>(TY) * kGradSplit) {
+                float dy[V], z[V], u[V], d[V], e[V];
+                load_run<T, V>(g.dy, row, col, n, dy);
+                if (GATED || act.value != DLF_ACT_NONE) load_run<T, V>(g.z, row, col, n, z);
+                if (GATED) load_run<T, V>(g.u, row, col, n, u);
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    const float2 a = act_grad_f<act.value>(GATED || act.value != DLF_ACT_NONE ? z[i] : 0.0f);
+                    d[i] = GATED ? dy[i] * u[i] * a.y : dy[i] * a.y;
+                    s0[i] += d[i];
+                    if (GATED) {
+                        e[i] = dy[i] * a.x;
+                        s1[i] += e[i];
+                    }
+                }
+                store_run<T, V>(g.d0, row, col, n, d);
+                if (GATED) store_run<T, V>(g.d1, row, col, n, e);
+                else store_run<T, V>(g.d0c, row, col, n, d);
+            }
+        });
+    if (!g.db0 && !g.db1) return;   // (the same for every thread of the cluster)
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        red[0][ty][tx * V + i] = s0[i];
+        if (GATED) red[GATED ? 1 : 0][ty][tx * V + i] = s1[i];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < (GATED ? 2 : 1) * kGradCols; i += kGradThreads) {
+        const int which = i / kGradCols, c = i % kGradCols;
+        float s = 0.0f;
+        for (int y = 0; y < TY; y++) s += red[which][y][c];
+        red[which][0][c] = s;
+    }
+    cluster.sync();
+    if (rank == 0)
+        for (int i = threadIdx.x; i < (GATED ? 2 : 1) * kGradCols; i += kGradThreads) {
+            const int which = i / kGradCols, c = i % kGradCols;
+            float s = 0.0f;
+            for (int r = 0; r < kGradSplit; r++) s += *cluster.map_shared_rank(&red[which][0][c], r);
+            float* db = which ? g.db1 : g.db0;
+            if (db && strip * kGradCols + c < g.N) db[strip * kGradCols + c] = s;
+        }
+    cluster.sync();   // no CTA leaves while its sums are still read
+}
+
+// ---- arguments -------------------------------------------------------------------------------------------------------------
+constexpr int64_t kMaxDim = 1ll << 30, kMaxLd = 1ll << 36;
+
+int check_sizes(int dtype, int act, int64_t m, int64_t k, int64_t n) {
+    if (dtype != DLF_F16 && dtype != DLF_BF16) return DLF_E_INVALID_ARG;
+    if (act < DLF_ACT_NONE || act > DLF_ACT_SILU) return DLF_E_INVALID_ARG;
+    if (m < 0 || k < 1 || n < 1 || m > kMaxDim || k > kMaxDim || n > kMaxDim) return DLF_E_SHAPE;
+    return DLF_OK;
+}
+
+// Collects a call's matrices: the first thing that is wrong with one of them, and their normalised form (the row length of a
+// matrix of one row is nobody's business).
+struct Mats {
+    int rc = DLF_OK;
+    Mat operator()(const void* p, int64_t rows, int64_t cols, int64_t ld, bool required) {
+        if (!p) {
+            if (required && rc == DLF_OK) rc = DLF_E_INVALID_ARG;
+            return Mat{nullptr, 0};
+        }
+        if (rc == DLF_OK && !aligned(2, p)) rc = DLF_E_INVALID_ARG;
+        if (rows <= 1) ld = (cols + 7) / 8 * 8;
+        if (rc == DLF_OK && (ld < cols || ld > kMaxLd)) rc = DLF_E_SHAPE;
+        return Mat{p, ld};
+    }
+    const float* vec(const float* p) {
+        if (rc == DLF_OK && !aligned(4, p)) rc = DLF_E_INVALID_ARG;
+        return p;
+    }
+};
+
+// Hands out 256-byte aligned pieces of a workspace; with a null base it only counts.
+struct Carver {
+    unsigned char* base;
+    size_t used = 0;
+    void* operator()(size_t bytes) {
+        void* p = base ? base + used : nullptr;
+        used += (bytes + 255) / 256 * 256;
+        return p;
+    }
+    Mat matrix(int64_t rows, int64_t cols) {
+        const int64_t ld = (cols + 7) / 8 * 8;
+        return Mat{(*this)(static_cast<size_t>(rows) * ld * 2), ld};
+    }
+};
+
+int check_workspace(const void* ws, size_t bytes, size_t need) {
+    if (need == 0) return DLF_OK;
+    return ws && bytes >= need && aligned(256, ws) ? DLF_OK : DLF_E_WORKSPACE;
+}
+
+int zero_matrix(const Mat& m, int64_t rows, int64_t cols, cudaStream_t s) {
+    if (!m.p) return DLF_OK;
+    const cudaError_t e = cudaMemset2DAsync(const_cast<void*>(m.p), static_cast<size_t>(m.ld) * 2, 0, static_cast<size_t>(cols) * 2, static_cast<size_t>(rows), s);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
+int zero_vec(float* p, int64_t n, cudaStream_t s) {
+    if (!p) return DLF_OK;
+    const cudaError_t e = cudaMemsetAsync(p, 0, static_cast<size_t>(n) * 4, s);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
+
+int launch_gemm(const DenseGemm& g, cudaStream_t s) { return launch_dense_simt(g, s); }
+
+// ---- the four operators; with `need` they only say how much workspace they want ------------------------------------------------
+int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+    if (!a) return DLF_E_INVALID_ARG;
+    int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
+    if (rc) return rc;
+    Mats mat;
+    DenseGemm g{};
+    g.dtype = a->dtype; g.act = a->act;
+    g.M = a->m; g.N = a->n; g.K = a->k;
+    g.sources = g.groups = 1;
+    g.a[0] = mat(a->x, a->m, a->k, a->ldx, a->m > 0);
+    g.b[0] = mat(a->w, a->n, a->k, a->ldw, true);
+    g.bias[0] = mat.vec(a->bias);
+    g.res = mat(a->res, a->m, a->n, a->ldres, false);
+    g.out[0] = mat(a->y, a->m, a->n, a->ldy, a->m > 0);
+    g.out[1] = mat(a->z, a->m, a->n, a->ldz, false);
+    if (mat.rc) return mat.rc;
+    Carver carve{static_cast<unsigned char*>(ws)};
+    if (need) { *need = carve.used; return DLF_OK; }
+    if (a->m == 0) return DLF_OK;
+    rc = check_workspace(ws, ws_bytes, carve.used);
+    return rc ? rc : launch_gemm(g, s);
+}
+
+int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+    if (!a) return DLF_E_INVALID_ARG;
+    int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
+    if (rc) return rc;
+    const bool has_act = a->act != DLF_ACT_NONE, some = a->m > 0;
+    Mats mat;
+    const Mat dy = mat(a->dy, a->m, a->n, a->lddy, some), x = mat(a->x, a->m, a->k, a->ldx, some && a->dw);
+    const Mat w = mat(a->w, a->n, a->k, a->ldw, some && a->dx), z = mat(a->z, a->m, a->n, a->ldz, some && has_act);
+    const Mat dx = mat(a->dx, a->m, a->k, a->lddx, false), dw = mat(a->dw, a->n, a->k, a->lddw, false);
+    const Mat dz_out = mat(a->dz, a->m, a->n, a->lddz, false);
+    float* db = const_cast<float*>(mat.vec(a->db));
+    if (mat.rc) return mat.rc;
+    Carver carve{static_cast<unsigned char*>(ws)};
+    // dz, as the products read it: dy itself where nothing lies between, else a matrix of its own
+    const bool products = dx.p || dw.p;
+    Mat dz = dy;
+    if (has_act && products) dz = dz_out.p ? dz_out : carve.matrix(a->m, a->n);
+    if (need) { *need = carve.used; return DLF_OK; }
+    if (!some) {
+        rc = zero_matrix(dw, a->n, a->k, s);
+        return rc ? rc : zero_vec(db, a->n, s);
+    }
+    rc = check_workspace(ws, ws_bytes, carve.used);
+    if (rc) return rc;
+    if ((has_act && products) || dz_out.p || db) {
+        DenseGrad d{};
+        d.dtype = a->dtype; d.act = a->act;
+        d.M = a->m; d.N = a->n;
+        d.dy = dy; d.z = z;
+        if (has_act && products) d.d0 = dz;
+        if (dz_out.p != d.d0.p) d.d0c = dz_out;
+        d.db0 = db;
+        rc = launch_dense_grad(d, s);
+        if (rc) return rc;
+    }
+    DenseGemm g{};
+    g.dtype = a->dtype; g.act = DLF_ACT_NONE;
+    g.sources = g.groups = 1;
+    if (dx.p) {   // dx[m][k] = sum over n of dz[m][n] w[n][k]
+        g.M = a->m; g.N = a->k; g.K = a->n;
+        g.a[0] = dz; g.b[0] = w; g.a_mn = false; g.b_mn = true;
+        g.out[0] = dx;
+        rc = launch_gemm(g, s);
+        if (rc) return rc;
+    }
+    if (dw.p) {   // dw[n][k] = sum over m of dz[m][n] x[m][k]
+        g.M = a->n; g.N = a->k; g.K = a->m;
+        g.a[0] = dz; g.b[0] = x; g.a_mn = true; g.b_mn = true;
+        g.out[0] = dw;
+        rc = launch_gemm(g, s);
+    }
+    return rc;
+}
+
+int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+    if (!a) return DLF_E_INVALID_ARG;
+    int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
+    if (rc) return rc;
+    Mats mat;
+    DenseGemm g{};
+    g.dtype = a->dtype; g.act = a->act;
+    g.M = a->m; g.N = a->n; g.K = a->k;
+    g.sources = g.groups = 1;
+    g.gated = true;
+    g.a[0] = mat(a->x, a->m, a->k, a->ldx, a->m > 0);
+    g.b[0] = mat(a->wg, a->n, a->k, a->ldwg, true);
+    g.b[1] = mat(a->wu, a->n, a->k, a->ldwu, true);
+    g.bias[0] = mat.vec(a->bg);
+    g.bias[1] = mat.vec(a->bu);
+    g.out[0] = mat(a->h, a->m, a->n, a->ldh, a->m > 0);
+    g.out[1] = mat(a->g, a->m, a->n, a->ldg, false);
+    g.out[2] = mat(a->u, a->m, a->n, a->ldu, false);
+    if (mat.rc) return mat.rc;
+    Carver carve{static_cast<unsigned char*>(ws)};
+    if (need) { *need = carve.used; return DLF_OK; }
+    if (a->m == 0) return DLF_OK;
+    rc = check_workspace(ws, ws_bytes, carve.used);
+    return rc ? rc : launch_gemm(g, s);
+}
+
+int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+    if (!a) return DLF_E_INVALID_ARG;
+    int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
+    if (rc) return rc;
+    const bool some = a->m > 0, any_dw = a->dwg || a->dwu;
+    Mats mat;
+    DenseGrad d{};
+    d.dtype = a->dtype; d.act = a->act;
+    d.M = a->m; d.N = a->n;
+    d.gated = true;
+    d.dy = mat(a->dh, a->m, a->n, a->lddh, some);
+    d.z = mat(a->g, a->m, a->n, a->ldg, some);
+    d.u = mat(a->u, a->m, a->n, a->ldu, some);
+    const Mat x = mat(a->x, a->m, a->k, a->ldx, some && any_dw);
+    const Mat wg = mat(a->wg, a->n, a->k, a->ldwg, some && a->dx), wu = mat(a->wu, a->n, a->k, a->ldwu, some && a->dx);
+    const Mat dx = mat(a->dx, a->m, a->k, a->lddx, false);
+    const Mat dwg = mat(a->dwg, a->n, a->k, a->lddwg, false), dwu = mat(a->dwu, a->n, a->k, a->lddwu, false);
+    d.db0 = const_cast<float*>(mat.vec(a->dbg));
+    d.db1 = const_cast<float*>(mat.vec(a->dbu));
+    if (mat.rc) return mat.rc;
+    Carver carve{static_cast<unsigned char*>(ws)};
+    if (dx.p || dwg.p) d.d0 = carve.matrix(a->m, a->n);
+    if (dx.p || dwu.p) d.d1 = carve.matrix(a->m, a->n);
+    if (need) { *need = carve.used; return DLF_OK; }
+    if (!some) {
+        rc = zero_matrix(dwg, a->n, a->k, s);
+        if (!rc) rc = zero_matrix(dwu, a->n, a->k, s);
+        if (!rc) rc = zero_vec(d.db0, a->n, s);
+        return rc ? rc : zero_vec(d.db1, a->n, s);
+    }
+    rc = check_workspace(ws, ws_bytes, carve.used);
+    if (rc) return rc;
+    rc = launch_dense_grad(d, s);
+    if (rc) return rc;
+    DenseGemm g{};
+    g.dtype = a->dtype; g.act = DLF_ACT_NONE;
+    if (dx.p) {   // dx = dg wg + du wu, one sum
+        g.sources = 2; g.groups = 1;
+        g.M = a->m; g.N = a->k; g.K = a->n;
+        g.a[0] = d.d0; g.a[1] = d.d1; g.b[0] = wg; g.b[1] = wu; g.a_mn = false; g.b_mn = true;
+        g.out[0] = dx;
+        rc = launch_gemm(g, s);
+        if (rc) return rc;
+    }
+    if (any_dw) {   // dwg = dg^T x and dwu = du^T x, one launch
+        g.sources = 1; g.groups = dwg.p && dwu.p ? 2 : 1;
+        g.M = a->n; g.N = a->k; g.K = a->m;
+        g.a[0] = dwg.p ? d.d0 : d.d1; g.a[1] = d.d1; g.b[0] = x; g.a_mn = true; g.b_mn = true;
+        g.out[0] = dwg.p ? dwg : dwu;
+        g.out[1] = g.groups > 1 ? dwu : Mat{nullptr, 0};
+        rc = launch_gemm(g, s);
+    }
+    return rc;
+}
+
+}  // namespace
+
+int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
+    auto vec = [](const Mat& m) { return !m.p || (aligned(16, m.p) && m.ld % 8 == 0); };
+    const bool v8 = vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
+    const int64_t blocks = (g.N + kGradCols - 1) / kGradCols * kGradSplit;   // (at most 2^27)
+    const int grid = static_cast<int>(blocks);
+    auto go = [&](auto kernel) {
+        const cudaError_t e = launch_kernel(kernel, grid, kGradThreads, 0, s, g);
+        return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+    };
+    if (g.dtype == DLF_BF16) {
+        if (g.gated) return v8 ? go(dense_grad_kernel<__nv_bfloat16, 8, true>) : go(dense_grad_kernel<__nv_bfloat16, 1, true>);
+        return v8 ? go(dense_grad_kernel<__nv_bfloat16, 8, false>) : go(dense_grad_kernel<__nv_bfloat16, 1, false>);
+    }
+    if (g.gated) return v8 ? go(dense_grad_kernel<__half, 8, true>) : go(dense_grad_kernel<__half, 1, true>);
+    return v8 ? go(dense_grad_kernel<__half, 8, false>) : go(dense_grad_kernel<__half, 1, false>);
+}
+
+}  // namespace dlf
+
+extern "C" {
+
+int dlf_linear_workspace_bytes(const dlf_linear_args* a, size_t* bytes) { return bytes ? dlf::linear(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
+int dlf_linear(const dlf_linear_args* a, void* workspace_dev, size_t bytes, void* stream) {
+    return dlf::linear(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
+}
+int dlf_linear_grad_workspace_bytes(const dlf_linear_grad_args* a, size_t* bytes) { return bytes ? dlf::linear_grad(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
+int dlf_linear_grad(const dlf_linear_grad_args* a, void* workspace_dev, size_t bytes, void* stream) {
+    return dlf::linear_grad(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
+}
+int dlf_gated_workspace_bytes(const dlf_gated_args* a, size_t* bytes) { return bytes ? dlf::gated(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
+int dlf_gated(const dlf_gated_args* a, void* workspace_dev, size_t bytes, void* stream) {
+    return dlf::gated(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
+}
+int dlf_gated_grad_workspace_bytes(const dlf_gated_grad_args* a, size_t* bytes) { return bytes ? dlf::gated_grad(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
+int dlf_gated_grad(const dlf_gated_grad_args* a, void* workspace_dev, size_t bytes, void* stream) {
+    return dlf::gated_grad(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
+}
+
+}  // extern "C"

@@ -1,0 +1,48 @@
+// Dense operators (dlf_linear*, dlf_gated*): what their host side hands to the kernels.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace dlf {
+
+// A row-major matrix of 16-bit values; ld = elements between the starts of two rows.
+struct Mat {
+    const void* p;
+    int64_t ld;
+};
+
+// D(m, n) = sum over k of A(m, k) B(n, k), summed in fp32 and finished by an epilogue.
+//   two sources:  D = A0 B0^T + A1 B1^T in one sum (the gradient of an input that two projections read)
+//   two groups:   D0 = A0 B0^T and D1 = A1 B0^T as one launch (the gradients of two weight matrices that read one input)
+//   gated:        G = A0 B0^T + bias0, U = A0 B1^T + bias1, out[0] = act(G) U, and G and U themselves to out[1] and out[2]
+//   otherwise:    out[0] = act(D + bias0 + res), and the sum itself to out[1]
+// a_mn, b_mn: the operand is stored the other way round, one row for each k.
+struct DenseGemm {
+    int dtype, act;
+    int64_t M, N, K;
+    int sources, groups;
+    bool gated, a_mn, b_mn;
+    Mat a[2], b[2];
+    const float* bias[2];
+    Mat res;
+    Mat out[3];
+};
+
+// Gradients behind an activation, element by element, and their sums over the rows in fp32 (of the values before rounding):
+//   gated:      d0 = dy u act'(z), d1 = dy act(z)        otherwise: d0 = dy act'(z)
+// d0c: d0 once more at another place.  Any output may be null.
+struct DenseGrad {
+    int dtype, act;
+    int64_t M, N;
+    bool gated;
+    Mat dy, z, u;
+    Mat d0, d1, d0c;
+    float *db0, *db1;
+};
+
+int launch_dense_simt(const DenseGemm& g, cudaStream_t s);
+int launch_dense_grad(const DenseGrad& g, cudaStream_t s);
+
+}  // namespace dlf
