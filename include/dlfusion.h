@@ -363,6 +363,10 @@ int dlf_gated_workspace_bytes(const dlf_gated_args* args, size_t* bytes);
 int dlf_gated(const dlf_gated_args* args, void* workspace_dev, size_t bytes, void* stream);
 int dlf_gated_grad_workspace_bytes(const dlf_gated_grad_args* args, size_t* bytes);
 int dlf_gated_grad(const dlf_gated_grad_args* args, void* workspace_dev, size_t bytes, void* stream);
+/* Waits for the stream and reports what went wrong with the dense operators' kernels: DLF_E_CUDA for a CUDA error, DLF_E_TIMEOUT if
+ * a bounded device-side wait gave up in any of them on the current device since the last such report (their outputs are then undefined).
+ * Not for streams that are being captured. */
+int dlf_dense_sync(void* stream);
 
 #ifdef __cplusplus
 }

@@ -113,6 +113,23 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
     cluster.sync();   // no CTA leaves while its sums are still read
 }
 
+// ---- rows onto 16-byte boundaries --------------------------------------------------------------------------------------------
+// For an operand whose rows start anywhere: the tensor-core kernels load tiles by TMA, which takes 16-byte boundaries only.  A copy costs
+// 4 bytes a value once, where a product reads the operand's tiles many times.
+__global__ void __launch_bounds__(256) dense_pack_kernel(const unsigned short* from, int64_t ld_from, uint4* to, int64_t ld_to8, int64_t rows, int64_t cols) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t per_row = (cols + 7) / 8, total = rows * per_row;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = i / per_row, c = (i - row * per_row) * 8;
+        const unsigned short* p = from + row * ld_from + c;
+        uint32_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = c + e < cols ? ld_map(p + e) : 0u;
+        to[row * ld_to8 + c / 8] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    }
+}
+
 // ---- arguments -------------------------------------------------------------------------------------------------------------
 constexpr int64_t kMaxDim = 1ll << 30, kMaxLd = 1ll << 36;
 
@@ -174,7 +191,25 @@ int zero_vec(float* p, int64_t n, cudaStream_t s) {
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
-int launch_gemm(const DenseGemm& g, cudaStream_t s) { return launch_dense_simt(g, s); }
+int launch_gemm(const DenseGemm& g, cudaStream_t s) { return launch_dense_pair(g, s); }
+
+// An operand as the products read it: itself, or a copy in the workspace (`run`: made now).
+struct Operands {
+    Carver& carve;
+    struct Copy { int64_t rows, cols; Mat from, to; } copies[4];
+    int n = 0;
+    Mat operator()(const Mat& m, int64_t rows, int64_t cols) {
+        if (!m.p || dense_rows16(m)) return m;
+        const Mat to = carve.matrix(rows, cols);
+        copies[n++] = Copy{rows, cols, m, to};
+        return to;
+    }
+    int run(cudaStream_t s) const {
+        int rc = DLF_OK;
+        for (int i = 0; i < n && rc == DLF_OK; i++) rc = launch_dense_pack(copies[i].rows, copies[i].cols, copies[i].from, copies[i].to, s);
+        return rc;
+    }
+};
 
 // ---- the four operators; with `need` they only say how much workspace they want ------------------------------------------------
 int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
@@ -193,10 +228,14 @@ int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, 
     g.out[0] = mat(a->y, a->m, a->n, a->ldy, a->m > 0);
     g.out[1] = mat(a->z, a->m, a->n, a->ldz, false);
     if (mat.rc) return mat.rc;
+    if (a->m == 0) { if (need) *need = 0; return DLF_OK; }
     Carver carve{static_cast<unsigned char*>(ws)};
+    Operands op{carve};
+    g.a[0] = op(g.a[0], a->m, a->k);
+    g.b[0] = op(g.b[0], a->n, a->k);
     if (need) { *need = carve.used; return DLF_OK; }
-    if (a->m == 0) return DLF_OK;
     rc = check_workspace(ws, ws_bytes, carve.used);
+    if (rc == DLF_OK) rc = op.run(s);
     return rc ? rc : launch_gemm(g, s);
 }
 
@@ -212,25 +251,30 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
     const Mat dz_out = mat(a->dz, a->m, a->n, a->lddz, false);
     float* db = const_cast<float*>(mat.vec(a->db));
     if (mat.rc) return mat.rc;
-    Carver carve{static_cast<unsigned char*>(ws)};
-    // dz, as the products read it: dy itself where nothing lies between, else a matrix of its own
-    const bool products = dx.p || dw.p;
-    Mat dz = dy;
-    if (has_act && products) dz = dz_out.p ? dz_out : carve.matrix(a->m, a->n);
-    if (need) { *need = carve.used; return DLF_OK; }
     if (!some) {
+        if (need) { *need = 0; return DLF_OK; }
         rc = zero_matrix(dw, a->n, a->k, s);
         return rc ? rc : zero_vec(db, a->n, s);
     }
+    Carver carve{static_cast<unsigned char*>(ws)};
+    Operands op{carve};
+    const Mat xo = dw.p ? op(x, a->m, a->k) : x, wo = dx.p ? op(w, a->n, a->k) : w;
+    // dz, as the products read it: dy itself where nothing lies between, the caller's dz, or a matrix of its own
+    const bool products = dx.p || dw.p;
+    Mat dz{nullptr, 0};
+    if (products) dz = !has_act && dense_rows16(dy) ? dy : dz_out.p && dense_rows16(dz_out) ? dz_out : carve.matrix(a->m, a->n);
+    if (need) { *need = carve.used; return DLF_OK; }
     rc = check_workspace(ws, ws_bytes, carve.used);
+    if (rc == DLF_OK) rc = op.run(s);
     if (rc) return rc;
-    if ((has_act && products) || dz_out.p || db) {
+    const bool own_dz = products && dz.p != dy.p;
+    if (own_dz || dz_out.p || db) {
         DenseGrad d{};
         d.dtype = a->dtype; d.act = a->act;
         d.M = a->m; d.N = a->n;
-        d.dy = dy; d.z = z;
-        if (has_act && products) d.d0 = dz;
-        if (dz_out.p != d.d0.p) d.d0c = dz_out;
+        d.dy = dy; d.z = has_act ? z : Mat{nullptr, 0};
+        if (own_dz) d.d0 = dz;
+        if (dz_out.p && dz_out.p != d.d0.p) d.d0c = dz_out;
         d.db0 = db;
         rc = launch_dense_grad(d, s);
         if (rc) return rc;
@@ -240,14 +284,14 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
     g.sources = g.groups = 1;
     if (dx.p) {   // dx[m][k] = sum over n of dz[m][n] w[n][k]
         g.M = a->m; g.N = a->k; g.K = a->n;
-        g.a[0] = dz; g.b[0] = w; g.a_mn = false; g.b_mn = true;
+        g.a[0] = dz; g.b[0] = wo; g.a_mn = false; g.b_mn = true;
         g.out[0] = dx;
         rc = launch_gemm(g, s);
         if (rc) return rc;
     }
     if (dw.p) {   // dw[n][k] = sum over m of dz[m][n] x[m][k]
         g.M = a->n; g.N = a->k; g.K = a->m;
-        g.a[0] = dz; g.b[0] = x; g.a_mn = true; g.b_mn = true;
+        g.a[0] = dz; g.b[0] = xo; g.a_mn = true; g.b_mn = true;
         g.out[0] = dw;
         rc = launch_gemm(g, s);
     }
@@ -273,10 +317,15 @@ int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, si
     g.out[1] = mat(a->g, a->m, a->n, a->ldg, false);
     g.out[2] = mat(a->u, a->m, a->n, a->ldu, false);
     if (mat.rc) return mat.rc;
+    if (a->m == 0) { if (need) *need = 0; return DLF_OK; }
     Carver carve{static_cast<unsigned char*>(ws)};
+    Operands op{carve};
+    g.a[0] = op(g.a[0], a->m, a->k);
+    g.b[0] = op(g.b[0], a->n, a->k);
+    g.b[1] = op(g.b[1], a->n, a->k);
     if (need) { *need = carve.used; return DLF_OK; }
-    if (a->m == 0) return DLF_OK;
     rc = check_workspace(ws, ws_bytes, carve.used);
+    if (rc == DLF_OK) rc = op.run(s);
     return rc ? rc : launch_gemm(g, s);
 }
 
@@ -300,17 +349,21 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     d.db0 = const_cast<float*>(mat.vec(a->dbg));
     d.db1 = const_cast<float*>(mat.vec(a->dbu));
     if (mat.rc) return mat.rc;
-    Carver carve{static_cast<unsigned char*>(ws)};
-    if (dx.p || dwg.p) d.d0 = carve.matrix(a->m, a->n);
-    if (dx.p || dwu.p) d.d1 = carve.matrix(a->m, a->n);
-    if (need) { *need = carve.used; return DLF_OK; }
     if (!some) {
+        if (need) { *need = 0; return DLF_OK; }
         rc = zero_matrix(dwg, a->n, a->k, s);
         if (!rc) rc = zero_matrix(dwu, a->n, a->k, s);
         if (!rc) rc = zero_vec(d.db0, a->n, s);
         return rc ? rc : zero_vec(d.db1, a->n, s);
     }
+    Carver carve{static_cast<unsigned char*>(ws)};
+    Operands op{carve};
+    const Mat xo = any_dw ? op(x, a->m, a->k) : x, wgo = dx.p ? op(wg, a->n, a->k) : wg, wuo = dx.p ? op(wu, a->n, a->k) : wu;
+    if (dx.p || dwg.p) d.d0 = carve.matrix(a->m, a->n);
+    if (dx.p || dwu.p) d.d1 = carve.matrix(a->m, a->n);
+    if (need) { *need = carve.used; return DLF_OK; }
     rc = check_workspace(ws, ws_bytes, carve.used);
+    if (rc == DLF_OK) rc = op.run(s);
     if (rc) return rc;
     rc = launch_dense_grad(d, s);
     if (rc) return rc;
@@ -319,7 +372,7 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     if (dx.p) {   // dx = dg wg + du wu, one sum
         g.sources = 2; g.groups = 1;
         g.M = a->m; g.N = a->k; g.K = a->n;
-        g.a[0] = d.d0; g.a[1] = d.d1; g.b[0] = wg; g.b[1] = wu; g.a_mn = false; g.b_mn = true;
+        g.a[0] = d.d0; g.a[1] = d.d1; g.b[0] = wgo; g.b[1] = wuo; g.a_mn = false; g.b_mn = true;
         g.out[0] = dx;
         rc = launch_gemm(g, s);
         if (rc) return rc;
@@ -327,7 +380,7 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     if (any_dw) {   // dwg = dg^T x and dwu = du^T x, one launch
         g.sources = 1; g.groups = dwg.p && dwu.p ? 2 : 1;
         g.M = a->n; g.N = a->k; g.K = a->m;
-        g.a[0] = dwg.p ? d.d0 : d.d1; g.a[1] = d.d1; g.b[0] = x; g.a_mn = true; g.b_mn = true;
+        g.a[0] = dwg.p ? d.d0 : d.d1; g.a[1] = d.d1; g.b[0] = xo; g.a_mn = true; g.b_mn = true;
         g.out[0] = dwg.p ? dwg : dwu;
         g.out[1] = g.groups > 1 ? dwu : Mat{nullptr, 0};
         rc = launch_gemm(g, s);
@@ -336,6 +389,17 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
 }
 
 }  // namespace
+
+int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to, cudaStream_t s) {
+    int sms = 0;
+    const int rc = query_sms(&sms);
+    if (rc) return rc;
+    const int64_t items = rows * ((cols + 7) / 8);
+    const int grid = static_cast<int>(std::min<int64_t>((items + 255) / 256, 8ll * sms));
+    const cudaError_t e = launch_kernel(dense_pack_kernel, grid, 256, 0, s, static_cast<const unsigned short*>(from.p), from.ld,
+                                        static_cast<uint4*>(const_cast<void*>(to.p)), to.ld / 8, rows, cols);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
 
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
     auto vec = [](const Mat& m) { return !m.p || (aligned(16, m.p) && m.ld % 8 == 0); };
@@ -357,6 +421,12 @@ int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
 }  // namespace dlf
 
 extern "C" {
+
+int dlf_dense_sync(void* stream) {
+    int code = 0;
+    const int rc = dlf::dense_pair_status(static_cast<cudaStream_t>(stream), &code);
+    return rc ? rc : code ? DLF_E_TIMEOUT : DLF_OK;
+}
 
 int dlf_linear_workspace_bytes(const dlf_linear_args* a, size_t* bytes) { return bytes ? dlf::linear(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
 int dlf_linear(const dlf_linear_args* a, void* workspace_dev, size_t bytes, void* stream) {

@@ -42,7 +42,12 @@ struct DenseGrad {
     float *db0, *db1;
 };
 
-int launch_dense_simt(const DenseGemm& g, cudaStream_t s);
+// True if a matrix can be a TMA operand: rows start on 16-byte boundaries.
+inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 0; }
+
+int launch_dense_pair(const DenseGemm& g, cudaStream_t s);    // dense_tc.cu; operands with rows on 16-byte boundaries
+int dense_pair_status(cudaStream_t s, int* code);             // waits for the stream; a kernel's bounded wait that gave up
+int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to, cudaStream_t s);
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s);
 
 }  // namespace dlf

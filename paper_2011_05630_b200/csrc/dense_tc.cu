@@ -1,0 +1,311 @@
+// Dense products on tcgen05 by CTA pairs: one persistent kernel for the forward products (with their epilogues) and the gradients'.
+//
+// A pair works on a 256 x BN tile of the result: either CTA loads its own 128 rows of A and half of B's rows, the tensor cores
+// of both read both halves of B (cta_group::2), so that an SM's shared memory takes in 32 KB per 64 of K for 2 * 128 * 256 * 64
+// operations (BN = 256) - half of what a CTA of its own would need.  One accumulator of BN columns of tensor memory is filled while the other
+// is drained.  A gated tile is the same product with the gate's 128 rows as one half of B and the up projection's as the other:
+// G and U of an output lie in the same lane, BN / 2 columns apart.
+//
+// Operands come as they lie in memory, along K or across it (the backward products read weights, inputs and gradients as the
+// forward pass left them; nothing is transposed): an operand across K arrives as boxes of 64 values of its other index by 64 of K.
+#include <cuda.h>
+
+#include <algorithm>
+#include <cstring>
+#include <type_traits>
+
+#include "dense.h"
+#include "dense_math.cuh"
+#include "dense_tc.cuh"
+
+namespace dlf {
+
+namespace {
+
+constexpr int kEpiWarps = 8;                // warps 0..7: warp & 3 = TMEM lane quarter, warp >> 2 = half of the columns
+constexpr int kAWarp = kEpiWarps, kBWarp = kAWarp + 1, kMmaWarp = kBWarp + 1;
+constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kRing = 192 * 1024;           // 6 stages of 32 KB, 8 of 24 KB
+constexpr int kStaging = kEpiWarps * 4096;  // 32 rows of 64 values for each epilogue warp
+constexpr int kDynSmem = kRing + kStaging + 1024;
+constexpr int kMaxStages = 8;
+enum { EPI_PLAIN = 0, EPI_LINEAR = 1, EPI_GATED = 2 };
+
+struct PairParams {
+    CUtensorMap a[2], b[2], out[3];
+    Mat o[3], res;                // (o: outputs without a tensor map, rows off the 16-byte boundaries)
+    const float* bias[2];
+    long long M, N, tiles, group_tiles;
+    int tiles_m, tiles_n;
+    int chunks1, chunks;          // 64-value chunks of K: of the first source, of both
+    int act, sources, groups;
+    bool out_tma[3], res_vec;
+};
+
+// Tiles are numbered along n within bands of kBand rows of tiles, so that the pairs at work at one time share operands.
+constexpr int kBand = 8;
+struct TileAt { int group; long long m0, n0; };
+template <int BN, int EPI>
+__device__ __forceinline__ TileAt tile_at(const PairParams& p, long long t) {
+    TileAt r;
+    r.group = p.groups > 1 && t >= p.group_tiles ? 1 : 0;
+    t -= r.group ? p.group_tiles : 0;
+    const long long per_band = static_cast<long long>(kBand) * p.tiles_n, band = t / per_band, in = t - band * per_band;
+    const int rows = min(kBand, p.tiles_m - static_cast<int>(band) * kBand);
+    const long long n = in / rows;
+    r.m0 = (band * kBand + (in - n * rows)) * 256;
+    r.n0 = n * (EPI == EPI_GATED ? BN / 2 : BN);
+    return r;
+}
+
+template <typename T, bool AMN, bool BMN, int EPI, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_pair_kernel(const __grid_constant__ PairParams p) {
+    constexpr int kABytes = 128 * 128, kBRows = BN / 2, kBBytes = kBRows * 128, kStageBytes = kABytes + kBBytes, kStages = kRing / kStageBytes;
+    static_assert(kStages <= kMaxStages, "ring");
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar[2], tempty_bar[2];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int abort_s;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* sbase = smem_raw + (base - smem_u32(smem_raw));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = static_cast<int>(cluster_rank());
+    volatile int* abort_flag = &abort_s;
+    int* status = &g_dense_status;
+    const long long t_first = blockIdx.x >> 1, t_step = gridDim.x >> 1;
+
+    if (warp == 0) {
+        if (lane == 0) abort_s = 0;
+        if (lane < kStages) {
+            mbar_init(&full_bar[lane], 2);    // the A and the B producer of the pair's first CTA, each with both CTAs' bytes
+            mbar_init(&empty_bar[lane], 1);
+        }
+        if (lane < 2) {
+            mbar_init(&tfull_bar[lane], 1);
+            mbar_init(&tempty_bar[lane], 2 * kEpiWarps);
+        }
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc_pair(&tmem_base_s, 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_arrive();   // both CTAs' barriers are initialised before either is signalled
+    cluster_wait();
+    tc_fence_after_sync();
+    pdl_launch_dependents();
+    pdl_wait();
+    const uint32_t tmem_base = tmem_base_s;
+
+    if (warp == kAWarp || warp == kBWarp) {
+        // ---- producers: one warp for A, one for B; the copies of a stage complete on the first CTA's barrier ----
+        const bool is_b = warp == kBWarp;
+        const int boxes = is_b ? (BMN ? kBRows / 64 : 1) : (AMN ? 2 : 1);
+        const uint32_t my_bytes = is_b ? kBBytes : kABytes;
+        int st = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (long long t = t_first; t < p.tiles && ok; t += t_step) {
+            const TileAt at = tile_at<BN, EPI>(p, t);
+            const int m0 = static_cast<int>(at.m0) + rank * 128, n0 = static_cast<int>(at.n0) + (EPI == EPI_GATED ? 0 : rank * kBRows);
+#pragma unroll 1
+            for (int c = 0; c < p.chunks; c++) {
+                ok = mbar_wait_warp(&empty_bar[st], ph ^ 1u, abort_flag, status, 0x100 | (blockIdx.x << 12));
+                if (!ok) break;
+                const bool second = c >= p.chunks1;
+                const int k0 = (second ? c - p.chunks1 : c) * 64;
+                if (lane == 0 && rank == 0) mbar_expect_tx(&full_bar[st], 2 * my_bytes);
+                __syncwarp();
+                if (lane < boxes) {
+                    const uint32_t bar = mapa(smem_u32(&full_bar[st]), 0);
+                    uint8_t* dst = sbase + st * kStageBytes + (is_b ? kABytes : 0) + lane * 8192;
+                    if (is_b) {
+                        const CUtensorMap* map = &p.b[EPI == EPI_GATED ? rank : (second ? 1 : 0)];
+                        if (BMN) tma_load_2d_pair(dst, map, bar, n0 + lane * 64, k0);
+                        else tma_load_2d_pair(dst, map, bar, k0, n0);
+                    } else {
+                        const CUtensorMap* map = &p.a[second || at.group ? 1 : 0];
+                        if (AMN) tma_load_2d_pair(dst, map, bar, m0 + lane * 64, k0);
+                        else tma_load_2d_pair(dst, map, bar, k0, m0);
+                    }
+                }
+                __syncwarp();
+                if (++st == kStages) { st = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        // ---- issuer: the pair's first CTA, the whole warp walks the loop, one elected lane issues ----
+        if (rank == 0) {
+            constexpr uint32_t idesc = dense_idesc<T>(256, BN, AMN, BMN);
+            const uint32_t a0 = AMN ? umma_desc_mn_lo(base, 8192) : umma_desc_lo(base);
+            const uint32_t b0 = BMN ? umma_desc_mn_lo(base + kABytes, 8192) : umma_desc_lo(base + kABytes);
+            int st = 0;
+            uint32_t ph = 0, j = 0;
+            bool ok = true;
+#pragma unroll 1
+            for (long long t = t_first; t < p.tiles && ok; t += t_step, j++) {
+                const uint32_t acc = j & 1u;
+                ok = mbar_wait_warp(&tempty_bar[acc], ((j >> 1) & 1u) ^ 1u, abort_flag, status, 0x200 | (blockIdx.x << 12));
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t d_tmem = tmem_base + acc * 256u;
+#pragma unroll 1
+                for (int c = 0; c < p.chunks; c++) {
+                    ok = mbar_wait_warp<true>(&full_bar[st], ph, abort_flag, status, 0x300 | (blockIdx.x << 12));
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t off = static_cast<uint32_t>(st) * (kStageBytes >> 4);
+                    if (elect_one()) {
+                        umma_chunk<2, AMN, BMN>(d_tmem, a0 + off, b0 + off, idesc, c != 0);
+                        umma_commit_pair(&empty_bar[st]);
+                    }
+                    __syncwarp();
+                    if (++st == kStages) { st = 0; ph ^= 1u; }
+                }
+                if (ok && elect_one()) umma_commit_pair(&tfull_bar[acc]);
+                __syncwarp();
+            }
+        }
+    } else {
+        // ---- epilogue: a lane holds a row of the tile; 64 columns at a time go through the warp's staging buffer (rows of 128
+        // bytes, swizzled as the tensor map expects, which also keeps the lanes' 16-byte writes apart) and leave as one TMA store ----
+        const int q = warp & 3, half = warp >> 2;
+        uint8_t* stg = sbase + kRing + warp * 4096;
+        constexpr int kChunks = EPI == EPI_GATED ? BN / 256 : BN / 128;   // of 64 output columns, for each warp
+        static_assert(kChunks >= 1, "tile");
+        uint32_t j = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (long long t = t_first; t < p.tiles && ok; t += t_step, j++) {
+            const TileAt at = tile_at<BN, EPI>(p, t);
+            const uint32_t acc = j & 1u;
+            const long long row0 = at.m0 + rank * 128 + q * 32, row = row0 + lane;
+            const uint32_t taddr = tmem_base + acc * 256u + (static_cast<uint32_t>(q * 32) << 16);
+#pragma unroll 1
+            for (int c = 0; c < kChunks; c++) {
+                const int cc = half * (kChunks * 64) + c * 64;      // column within the tile's outputs
+                const long long col0 = at.n0 + cc;
+                const int cols = static_cast<int>(max(0ll, min(64ll, p.N - col0)));
+                uint4 res[EPI == EPI_LINEAR ? 8 : 1];
+                if constexpr (EPI == EPI_LINEAR) {
+                    if (p.res.p) load_row64<T>(p.res, p.res_vec, row, col0, row < p.M ? cols : 0, res);
+                }
+                if (c == 0) {
+                    ok = mbar_wait_warp(&tfull_bar[acc], (j >> 1) & 1u, abort_flag, status, 0x400 | (blockIdx.x << 12));
+                    tc_fence_after_sync();
+                }
+                if (!ok) break;
+                float v[64];
+                tmem_ld32(taddr + cc, v);
+                tmem_ld32(taddr + cc + 32, v + 32);
+                [[maybe_unused]] float u[EPI == EPI_GATED ? 64 : 1];
+                if constexpr (EPI == EPI_GATED) {
+                    tmem_ld32(taddr + BN / 2 + cc, u);
+                    tmem_ld32(taddr + BN / 2 + cc + 32, u + 32);
+                }
+                if (c == kChunks - 1) {   // the accumulator has been read
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(mapa(smem_u32(&tempty_bar[acc]), 0));
+                }
+                if (cols == 0 || row0 >= p.M) continue;   // (the same for the whole warp)
+                auto put = [&](int which, const float* val) {
+                    store_rows64<T>(p.o[which], &p.out[which], p.out_tma[which], stg, lane, row0, col0, p.M, cols, val);
+                };
+                if constexpr (EPI == EPI_PLAIN) {
+                    put(at.group, v);
+                } else if constexpr (EPI == EPI_LINEAR) {
+                    if (p.bias[0]) add_bias64(p.bias[0], col0, cols, v);
+                    if (p.res.p) add_row64<T>(res, v);
+                    if (p.o[1].p) put(1, v);
+                    with_act(p.act, [&](auto act) {
+#pragma unroll
+                        for (int i = 0; i < 64; i++) v[i] = act_f<act.value>(v[i]);
+                    });
+                    put(0, v);
+                } else {
+                    if (p.bias[0]) add_bias64(p.bias[0], col0, cols, v);
+                    if (p.bias[1]) add_bias64(p.bias[1], col0, cols, u);
+                    if (p.o[1].p) put(1, v);
+                    if (p.o[2].p) put(2, u);
+                    with_act(p.act, [&](auto act) {
+#pragma unroll
+                        for (int i = 0; i < 64; i++) v[i] = act_f<act.value>(v[i]) * u[i];
+                    });
+                    put(0, v);
+                }
+            }
+        }
+        if (lane == 0) tma_store_wait_read();   // shared memory outlives every store that reads it
+        __syncwarp();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    // neither CTA leaves while the other may still read its operands or signal its barriers
+    cluster_arrive();
+    cluster_wait();
+    if (warp == kMmaWarp) {
+        if (abort_s) __nanosleep(20000);
+        tc_fence_after_sync();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
+typedef void (*PairFn)(const PairParams);
+template <typename T>
+PairFn pick_pair(const DenseGemm& g, int bn) {
+    if (g.gated) return dense_pair_kernel<T, false, false, EPI_GATED, 256>;
+    if (g.a_mn) return bn == 256 ? dense_pair_kernel<T, true, true, EPI_PLAIN, 256> : dense_pair_kernel<T, true, true, EPI_PLAIN, 128>;
+    if (g.b_mn) return bn == 256 ? dense_pair_kernel<T, false, true, EPI_PLAIN, 256> : dense_pair_kernel<T, false, true, EPI_PLAIN, 128>;
+    return bn == 256 ? dense_pair_kernel<T, false, false, EPI_LINEAR, 256> : dense_pair_kernel<T, false, false, EPI_LINEAR, 128>;
+}
+
+}  // namespace
+
+int launch_dense_pair(const DenseGemm& g, cudaStream_t s) {
+    int sms = 0;
+    int rc = query_sms(&sms);
+    if (rc) return rc;
+    PairParams p;
+    std::memset(&p, 0, sizeof(p));
+    int bn = 256;
+    auto count = [&](int b) { return ((g.M + 255) / 256) * ((g.N + (g.gated ? b / 2 : b) - 1) / (g.gated ? b / 2 : b)) * g.groups; };
+    if (!g.gated && (count(256) + sms / 2 - 1) / (sms / 2) * 2 > (count(128) + sms / 2 - 1) / (sms / 2)) bn = 128;
+    for (int i = 0; i < 2 && rc == DLF_OK; i++) {
+        const Mat &a = g.a[i].p ? g.a[i] : g.a[0], &b = g.b[i].p ? g.b[i] : g.b[0];
+        rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, 128, 64);
+        if (rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, bn / 2, 64);
+    }
+    for (int i = 0; i < 3 && rc == DLF_OK; i++) {
+        p.o[i] = g.out[i];
+        p.out_tma[i] = g.out[i].p && dense_rows16(g.out[i]);
+        if (p.out_tma[i]) rc = dense_map(&p.out[i], g.out[i], g.M, g.N, 32, 64);
+    }
+    if (rc) return rc;
+    p.res = g.res;
+    p.res_vec = dense_rows16(g.res);
+    p.bias[0] = g.bias[0]; p.bias[1] = g.bias[1];
+    p.M = g.M; p.N = g.N;
+    const int step = g.gated ? bn / 2 : bn;
+    p.tiles_m = static_cast<int>((g.M + 255) / 256);
+    p.tiles_n = static_cast<int>((g.N + step - 1) / step);
+    p.group_tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
+    p.tiles = p.group_tiles * g.groups;
+    p.chunks1 = static_cast<int>((g.K + 63) / 64);
+    p.chunks = p.chunks1 * g.sources;
+    p.act = g.act; p.sources = g.sources; p.groups = g.groups;
+    const int grid = 2 * static_cast<int>(std::min<long long>(p.tiles, sms / 2));
+    const PairFn fn = g.dtype == DLF_BF16 ? pick_pair<__nv_bfloat16>(g, bn) : pick_pair<__half>(g, bn);
+    rc = dense_smem_attr(reinterpret_cast<const void*>(fn), kDynSmem);
+    if (rc) return rc;
+    const cudaError_t e = launch_kernel(fn, grid, kThreads, kDynSmem, s, p);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
+
+int dense_pair_status(cudaStream_t s, int* code) { return dense_status_of(s, code); }
+
+}  // namespace dlf

@@ -1,0 +1,195 @@
+// What the tensor-core kernels of the dense operators share: tensor maps over row-major 16-bit matrices, products of a 64-value chunk
+// of K with operands along or across K, rows of 64 values between registers and memory, and the word that a wait which gave up
+// leaves its code in.
+#pragma once
+#include <cuda.h>
+
+#include <atomic>
+
+#include "dense.h"
+#include "dense_math.cuh"
+#include "ptx.cuh"
+
+namespace dlf {
+
+// One for each source file that includes this (see dense_status_of).
+static __device__ int g_dense_status;
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+// A map over a matrix of `rows` rows of `cols` values (any 16-bit type: the copies move bits), boxes of box_rows x box_cols.
+inline int dense_map(CUtensorMap* m, const Mat& a, int64_t rows, int64_t cols, int box_rows, int box_cols) {
+    const uint64_t dims[2] = {static_cast<uint64_t>(cols), static_cast<uint64_t>(rows)};
+    const uint64_t strides[1] = {static_cast<uint64_t>(a.ld) * 2};
+    const uint32_t box[2] = {static_cast<uint32_t>(box_cols), static_cast<uint32_t>(box_rows)}, es[2] = {1, 1};
+    return encode_tmap(m, a.p, 2, dims, strides, box, es);
+}
+
+// Raises a kernel's limit of dynamic shared memory once per device.
+inline int dense_smem_attr(const void* fn, int bytes) {
+    constexpr int kMax = 64;
+    static std::atomic<const void*> seen[kMaxDevices][kMax];
+    const int dev = current_device_slot();
+    if (dev < 0) return DLF_E_UNSUPPORTED;
+    int i = 0;
+    for (; i < kMax; i++) {
+        const void* f = seen[dev][i].load(std::memory_order_acquire);
+        if (f == fn) return DLF_OK;
+        if (!f) break;
+    }
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return cuda_fail(e);
+    const void* none = nullptr;
+    if (i < kMax) seen[dev][i].compare_exchange_strong(none, fn, std::memory_order_release);   // (lost to another thread: set again next time)
+    return DLF_OK;
+}
+
+// Waits for the stream and reads the status word; a code in it is reported once.
+inline int dense_status_of(cudaStream_t s, int* code) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(code, g_dense_status, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess) return cuda_fail(e);
+    if (*code) {
+        const int zero = 0;
+        e = cudaMemcpyToSymbolAsync(g_dense_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
+    return DLF_OK;
+}
+
+// ---- device ----------------------------------------------------------------------------------------------------------------
+// Instruction descriptor: fp16 or bf16 operands (bits 7 and 10), fp32 sums; bits 15 and 16: operand A, B across K.
+template <typename T>
+__host__ __device__ constexpr uint32_t dense_idesc(int m, int n, bool amn, bool bmn) {
+    return (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | (amn ? 1u << 15 : 0u) | (bmn ? 1u << 16 : 0u) |
+           (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+// The four K = 16 steps of a 64-value chunk in one statement.  Along K a step is 32 bytes further (2 units), across K two
+// 1024-byte atoms (128 units).
+#define DLF_DENSE_STEP(CG, S)                                                                                                  \
+    "mad.lo.u32 ta, %6, " #S ", %1;\n\tmad.lo.u32 tb, %7, " #S ", %2;\n\tmov.b64 da, {ta, %5};\n\tmov.b64 db, {tb, %5};\n\t"     \
+    "tcgen05.mma.cta_group::" #CG ".kind::f16 [%0], da, db, %3, p;\n\t"
+#define DLF_DENSE_CHUNK(CG)                                                                                                    \
+    "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t.reg .b32 ta, tb;\n\tsetp.ne.b32 p, %4, 0;\n\t" DLF_DENSE_STEP(CG, 0)             \
+    "setp.eq.b32 p, %3, %3;\n\t" DLF_DENSE_STEP(CG, 1) DLF_DENSE_STEP(CG, 2) DLF_DENSE_STEP(CG, 3) "}"
+template <int CG, bool AMN, bool BMN>
+__device__ __forceinline__ void umma_chunk(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    if (CG == 2)
+        asm volatile(DLF_DENSE_CHUNK(2)::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHiSw128), "n"(AMN ? 128 : 2), "n"(BMN ? 128 : 2) : "memory");
+    else
+        asm volatile(DLF_DENSE_CHUNK(1)::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHiSw128), "n"(AMN ? 128 : 2), "n"(BMN ? 128 : 2) : "memory");
+}
+#undef DLF_DENSE_STEP
+#undef DLF_DENSE_CHUNK
+
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(src)), "r"(c0), "r"(c1) : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    T v[2] = {from_f32<T>(a), from_f32<T>(b)};
+    return *reinterpret_cast<const uint32_t*>(v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The first `cols` (0 to 64) values of a row from column col0 on, as they lie in memory; zeros behind them.
+template <typename T>
+__device__ __forceinline__ void load_row64(const Mat& m, bool vec, int64_t row, int64_t col0, int cols, uint4 (&q)[8]) {
+    const T* p = static_cast<const T*>(m.p) + row * m.ld + col0;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        q[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (vec && j * 8 + 8 <= cols) {
+            q[j] = ld_map(reinterpret_cast<const uint4*>(p + j * 8));
+        } else if (j * 8 < cols) {
+            const unsigned short* e = reinterpret_cast<const unsigned short*>(p + j * 8);
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t lo = j * 8 + 2 * i < cols ? ld_map(e + 2 * i) : 0u, hi = j * 8 + 2 * i + 1 < cols ? ld_map(e + 2 * i + 1) : 0u;
+                w[i] = lo | hi << 16;
+            }
+            q[j] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void add_row64(const uint4 (&q)[8], float* v) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const T* e = reinterpret_cast<const T*>(&q[j]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[j * 8 + i] += to_f32(e[i]);
+    }
+}
+__device__ __forceinline__ void add_bias64(const float* bias, int64_t col0, int cols, float* v) {
+    const float* b = bias + col0;
+    if (cols == 64 && (reinterpret_cast<uintptr_t>(b) & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const float4 f = ld_map(reinterpret_cast<const float4*>(b) + i);
+            v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 64; i++)
+            if (i < cols) v[i] += ld_map(b + i);
+    }
+}
+
+// A warp's 32 rows of 64 values (a lane holds a row): rounded, through `stg` (4096 bytes of the warp's own) and out, by a TMA store
+// where the output has a map, else row by row.  Rows and columns beyond the matrix are not written.  (A TMA store clips at the map's
+// edge in pieces of 16 bytes: with a last piece that is not whole it writes zeros behind the row's end.)
+template <typename T>
+__device__ __forceinline__ void store_rows64(const Mat& o, const CUtensorMap* map, bool tma, uint8_t* stg, int lane, int64_t row0, int64_t col0,
+                                             int64_t rows_end, int cols, const float* v) {
+    if (lane == 0) tma_store_wait_read();   // what lay here before has left
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const uint4 q = make_uint4(pack2<T>(v[8 * j], v[8 * j + 1]), pack2<T>(v[8 * j + 2], v[8 * j + 3]), pack2<T>(v[8 * j + 4], v[8 * j + 5]),
+                                   pack2<T>(v[8 * j + 6], v[8 * j + 7]));
+        *reinterpret_cast<uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) = q;
+    }
+    if (tma && (cols & 7) == 0) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(map, stg, static_cast<int>(col0), static_cast<int>(row0));
+            tma_store_commit();
+        }
+    } else {
+        __syncwarp();
+        const int rows = static_cast<int>(min(static_cast<int64_t>(32), rows_end - row0));
+        T* p = static_cast<T*>(const_cast<void*>(o.p)) + row0 * o.ld + col0;
+        for (int r = 0; r < rows; r++, p += o.ld)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int c = lane + h * 32;
+                if (c < cols) p[c] = *reinterpret_cast<const T*>(stg + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2);
+            }
+        __syncwarp();
+    }
+}
+
+}  // namespace dlf

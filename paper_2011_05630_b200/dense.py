@@ -75,6 +75,12 @@ def _call(op, args, device, ask):
         raise B.DlfError(status, op)
 
 
+def synchronize(device=None):
+    """Waits for the current stream; raises if a dense operator's kernel on the device gave up (see dlf_dense_sync)."""
+    with torch.cuda.device(device):
+        B._check(B.lib().dlf_dense_sync(torch.cuda.current_stream().cuda_stream), "dlf_dense_sync")
+
+
 def _out(out, name, rows, cols, like):
     return torch.empty((rows, cols), dtype=like.dtype, device=like.device) if out is None else out
 

@@ -143,6 +143,17 @@ def test_strides(size, pads, shift):
     check_gated_backward(mk, *size, "silu", True, pads, shift)
 
 
+@pytest.mark.parametrize("size", [(1, 250, 130), (10, 250, 130), (48, 122, 258), (300, 506, 1002)], ids=str)
+def test_rows_that_end_inside_16_bytes(size):
+    """Rows that start on 16-byte boundaries and end between two, NaN behind them."""
+    mk, pads = Maker(sum(size), torch.bfloat16), (6, 6, 6)
+    check_linear(mk, *size, "gelu", True, True, True, pads)
+    check_linear_backward(mk, *size, "gelu", True, True, pads)
+    check_linear_backward(mk, *size, "none", True, True, pads)
+    check_gated(mk, *size, "silu", True, True, pads)
+    check_gated_backward(mk, *size, "silu", True, pads)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
 @pytest.mark.parametrize("size", [(1, 512, 300), (8, 1000, 264), (24, 1100, 530), (130, 640, 300), (515, 600, 1000)], ids=str)
 def test_exact_sums(size, dtype):
