@@ -191,7 +191,43 @@ int zero_vec(float* p, int64_t n, cudaStream_t s) {
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
-int launch_gemm(const DenseGemm& g, cudaStream_t s) { return launch_dense_pair(g, s); }
+// SM clocks that the kernel of dense_lat.cu would take, and its best layout.
+double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
+    double least = -1.0;
+    const int64_t tiles_m = (g.M + 127) / 128;
+    DenseLatChoice c;
+    c.rows = g.a_mn ? static_cast<int>(std::min<int64_t>(g.M, 128)) : static_cast<int>((g.M + tiles_m - 1) / tiles_m);
+    const int64_t chunks = (g.K + 63) / 64 * g.sources;
+    for (c.bn = 64; c.bn <= 128; c.bn += 64) {
+        const int step = g.gated ? c.bn / 2 : c.bn;
+        const int64_t tiles = tiles_m * ((g.N + step - 1) / step) * g.groups;
+        for (c.split = 1; c.split <= 8; c.split *= 2) {
+            if (tiles * c.split > (1 << 20) || !dense_lat_possible(g, c)) continue;
+            const double stage = (g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024) + c.bn * 128;
+            const double share = static_cast<double>((chunks + c.split - 1) / c.split), waves = static_cast<double>((tiles * c.split + sms - 1) / sms);
+            const double cost = 3000.0 + waves * (share * std::max(stage / 57.0, 330.0) + (c.split > 1 ? 2000.0 : 0.0) + c.rows * c.bn * 0.2);
+            if (least < 0 || cost < least) {
+                least = cost;
+                *best = c;
+            }
+        }
+    }
+    return least;
+}
+double pair_cost(const DenseGemm& g, int sms) {
+    const int step = g.gated ? 128 : 256;
+    const int64_t tiles = (g.M + 255) / 256 * ((g.N + step - 1) / step) * g.groups, pairs = sms / 2;
+    return 5000.0 + static_cast<double>((tiles + pairs - 1) / pairs) * static_cast<double>((g.K + 63) / 64 * g.sources) * 540.0 + 3000.0;
+}
+
+int launch_gemm(const DenseGemm& g, cudaStream_t s) {
+    int sms = 0;
+    const int rc = query_sms(&sms);
+    if (rc) return rc;
+    DenseLatChoice c{};
+    const double lat = lat_cost(g, sms, &c);
+    return lat >= 0 && lat < pair_cost(g, sms) ? launch_dense_lat(g, c, s) : launch_dense_pair(g, s);
+}
 
 // An operand as the products read it: itself, or a copy in the workspace (`run`: made now).
 struct Operands {
@@ -424,7 +460,12 @@ extern "C" {
 
 int dlf_dense_sync(void* stream) {
     int code = 0;
-    const int rc = dlf::dense_pair_status(static_cast<cudaStream_t>(stream), &code);
+    int rc = dlf::dense_pair_status(static_cast<cudaStream_t>(stream), &code);
+    if (rc == DLF_OK) {
+        int lat = 0;
+        rc = dlf::dense_lat_status(static_cast<cudaStream_t>(stream), &lat);
+        code |= lat;
+    }
     return rc ? rc : code ? DLF_E_TIMEOUT : DLF_OK;
 }
 

@@ -47,6 +47,15 @@ inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 
 
 int launch_dense_pair(const DenseGemm& g, cudaStream_t s);    // dense_tc.cu; operands with rows on 16-byte boundaries
 int dense_pair_status(cudaStream_t s, int* code);             // waits for the stream; a kernel's bounded wait that gave up
+// dense_lat.cu: tiles of `rows` rows (at most 128) by `bn` columns of B (64 or 128; both halves of a gated tile), K shared out over
+// `split` CTAs (1, 2, 4, 8).
+struct DenseLatChoice {
+    int rows, bn, split;
+};
+bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c);
+int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s);
+int dense_lat_status(cudaStream_t s, int* code);
+
 int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to, cudaStream_t s);
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s);
 

@@ -120,16 +120,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
                 const int k0 = (second ? c - p.chunks1 : c) * 64;
                 if (lane == 0 && rank == 0) mbar_expect_tx(&full_bar[st], 2 * my_bytes);
                 __syncwarp();
-                if (lane < boxes) {
+                const int bx = lane - boxes * st;   // (another lane for every stage: the copies of one thread run one after the other)
+                if (bx >= 0 && bx < boxes) {
                     const uint32_t bar = mapa(smem_u32(&full_bar[st]), 0);
-                    uint8_t* dst = sbase + st * kStageBytes + (is_b ? kABytes : 0) + lane * 8192;
+                    uint8_t* dst = sbase + st * kStageBytes + (is_b ? kABytes : 0) + bx * 8192;
                     if (is_b) {
                         const CUtensorMap* map = &p.b[EPI == EPI_GATED ? rank : (second ? 1 : 0)];
-                        if (BMN) tma_load_2d_pair(dst, map, bar, n0 + lane * 64, k0);
+                        if (BMN) tma_load_2d_pair(dst, map, bar, n0 + bx * 64, k0);
                         else tma_load_2d_pair(dst, map, bar, k0, n0);
                     } else {
                         const CUtensorMap* map = &p.a[second || at.group ? 1 : 0];
-                        if (AMN) tma_load_2d_pair(dst, map, bar, m0 + lane * 64, k0);
+                        if (AMN) tma_load_2d_pair(dst, map, bar, m0 + bx * 64, k0);
                         else tma_load_2d_pair(dst, map, bar, k0, m0);
                     }
                 }
@@ -274,7 +275,8 @@ int launch_dense_pair(const DenseGemm& g, cudaStream_t s) {
     std::memset(&p, 0, sizeof(p));
     int bn = 256;
     auto count = [&](int b) { return ((g.M + 255) / 256) * ((g.N + (g.gated ? b / 2 : b) - 1) / (g.gated ? b / 2 : b)) * g.groups; };
-    if (!g.gated && (count(256) + sms / 2 - 1) / (sms / 2) * 2 > (count(128) + sms / 2 - 1) / (sms / 2)) bn = 128;
+    // (a tile of half the width takes 0.9 of the time: its 24 KB per 64 of K come no faster)
+    if (!g.gated && (count(256) + sms / 2 - 1) / (sms / 2) * 10 > (count(128) + sms / 2 - 1) / (sms / 2) * 9) bn = 128;
     for (int i = 0; i < 2 && rc == DLF_OK; i++) {
         const Mat &a = g.a[i].p ? g.a[i] : g.a[0], &b = g.b[i].p ? g.b[i] : g.b[0];
         rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, 128, 64);
