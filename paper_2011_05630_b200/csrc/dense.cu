@@ -21,38 +21,36 @@ namespace {
 // atomics and no second kernel.
 constexpr int kGradCols = 64, kGradThreads = 256, kGradSplit = 8;
 
+// V values of a row, as they lie in memory; those behind the row's end (n of them exist) are zero and stay unwritten.
 template <typename T, int V>
-__device__ __forceinline__ void load_run(const Mat& m, int64_t row, int64_t col, int n, float (&v)[V]) {
-    const T* p = static_cast<const T*>(m.p) + row * m.ld + col;
-    if (V == 8 && n == 8) {
-        const uint4 q = ld_map(reinterpret_cast<const uint4*>(p));
-        const T* e = reinterpret_cast<const T*>(&q);
+struct alignas(V * 2) Run {
+    T v[V];
+    __device__ __forceinline__ float get(int i) const { return to_f32(v[i]); }
+    __device__ __forceinline__ void set(int i, float f) { v[i] = from_f32<T>(f); }
+    __device__ __forceinline__ void load(const Mat& m, int64_t row, int64_t col, int n) {
+        const T* p = static_cast<const T*>(m.p) + row * m.ld + col;
+        if (V == 8 && n == 8) {
+            *reinterpret_cast<uint4*>(v) = ld_map(reinterpret_cast<const uint4*>(p));
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; i++) v[i] = to_f32(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i++) v[i] = i < n ? to_f32(ld_map(p + i)) : 0.0f;
+            for (int i = 0; i < V; i++) v[i] = i < n ? ld_map(p + i) : from_f32<T>(0.0f);
+        }
     }
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_run(const Mat& m, int64_t row, int64_t col, int n, const float (&v)[V]) {
-    if (!m.p) return;
-    T* p = static_cast<T*>(const_cast<void*>(m.p)) + row * m.ld + col;
-    if (V == 8 && n == 8) {
-        uint4 q;
-        T* e = reinterpret_cast<T*>(&q);
+    __device__ __forceinline__ void store(const Mat& m, int64_t row, int64_t col, int n) const {
+        if (!m.p) return;
+        T* p = static_cast<T*>(const_cast<void*>(m.p)) + row * m.ld + col;
+        if (V == 8 && n == 8) {
+            *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v);
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; i++) e[i] = from_f32<T>(v[i]);
-        *reinterpret_cast<uint4*>(p) = q;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i++)
-            if (i < n) p[i] = from_f32<T>(v[i]);
+            for (int i = 0; i < V; i++)
+                if (i < n) p[i] = v[i];
+        }
     }
-}
+};
 
 template <typename T, int V, bool GATED>
-__global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThreads) dense_grad_kernel(const __grid_constant__ DenseGrad g) {
+__global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThreads, GATED ? 2 : 3) dense_grad_kernel(const __grid_constant__ DenseGrad g) {
     constexpr int TX = kGradCols / V, TY = kGradThreads / TX;
     __shared__ float red[GATED ? 2 : 1][TY][kGradCols];
     pdl_wait();
@@ -64,30 +62,47 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
     const int64_t col = strip * kGradCols + tx * V;
     const int n = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(V), g.N - col)));
     float s0[V] = {}, s1[V] = {};
+    // rows are dealt out round by round, so that the CTAs of a strip are never far apart; kRows of a thread's rows are on their way at
+    // a time
+    constexpr int kRows = V == 8 ? 4 : 8;
+    constexpr int64_t kStep = static_cast<int64_t>(TY) * kGradSplit;
+    const bool with_z = GATED || g.act != DLF_ACT_NONE;
     if (n > 0)
-        with_act(g.act, [&](auto act) {
-            // (rows are dealt out round by round, so that the CTAs of a strip are never more than TY rows of work apart)
-#pragma unroll 2
-            for (int64_t row = static_cast<int64_t>(rank) * TY + ty; row < g.M; row += static_cast<int64_t>(TY) * kGradSplit) {
-                float dy[V], z[V], u[V], d[V], e[V];
-                load_run<T, V>(g.dy, row, col, n, dy);
-                if (GATED || act.value != DLF_ACT_NONE) load_run<T, V>(g.z, row, col, n, z);
-                if (GATED) load_run<T, V>(g.u, row, col, n, u);
+#pragma unroll 1
+        for (int64_t row0 = static_cast<int64_t>(rank) * TY + ty; row0 < g.M; row0 += kRows * kStep) {
+            Run<T, V> dy[kRows], z[kRows], u[GATED ? kRows : 1];
 #pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const float2 a = act_grad_f<act.value>(GATED || act.value != DLF_ACT_NONE ? z[i] : 0.0f);
-                    d[i] = GATED ? dy[i] * u[i] * a.y : dy[i] * a.y;
-                    s0[i] += d[i];
-                    if (GATED) {
-                        e[i] = dy[i] * a.x;
-                        s1[i] += e[i];
-                    }
-                }
-                store_run<T, V>(g.d0, row, col, n, d);
-                if (GATED) store_run<T, V>(g.d1, row, col, n, e);
-                else store_run<T, V>(g.d0c, row, col, n, d);
+            for (int r = 0; r < kRows; r++) {
+                const int64_t row = row0 + r * kStep;
+                if (row >= g.M) break;
+                dy[r].load(g.dy, row, col, n);
+                if (with_z) z[r].load(g.z, row, col, n);
+                if (GATED) u[GATED ? r : 0].load(g.u, row, col, n);
             }
-        });
+            with_act(g.act, [&](auto act) {
+#pragma unroll
+                for (int r = 0; r < kRows; r++) {
+                    const int64_t row = row0 + r * kStep;
+                    if (row >= g.M) break;
+                    Run<T, V> d, e;
+#pragma unroll
+                    for (int i = 0; i < V; i++) {
+                        const float2 a = act_grad_f<act.value>(GATED || act.value != DLF_ACT_NONE ? z[r].get(i) : 0.0f);
+                        const float t = dy[r].get(i);
+                        const float v = GATED ? t * u[GATED ? r : 0].get(i) * a.y : t * a.y;
+                        s0[i] += v;
+                        d.set(i, v);
+                        if (GATED) {
+                            s1[i] += t * a.x;
+                            e.set(i, t * a.x);
+                        }
+                    }
+                    d.store(g.d0, row, col, n);
+                    if (GATED) e.store(g.d1, row, col, n);
+                    else d.store(g.d0c, row, col, n);
+                }
+            });
+        }
     if (!g.db0 && !g.db1) return;   // (the same for every thread of the cluster)
 #pragma unroll
     for (int i = 0; i < V; i++) {
@@ -264,7 +279,9 @@ int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, 
     g.out[0] = mat(a->y, a->m, a->n, a->ldy, a->m > 0);
     g.out[1] = mat(a->z, a->m, a->n, a->ldz, false);
     if (mat.rc) return mat.rc;
-    if (a->m == 0) { if (need) *need = 0; return DLF_OK; }
+    if (need) *need = 0;
+    if (a->m == 0) return DLF_OK;
+    if (dense_gemv_takes(a->m)) return need ? DLF_OK : launch_dense_gemv(g, s);
     Carver carve{static_cast<unsigned char*>(ws)};
     Operands op{carve};
     g.a[0] = op(g.a[0], a->m, a->k);
@@ -353,7 +370,9 @@ int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, si
     g.out[1] = mat(a->g, a->m, a->n, a->ldg, false);
     g.out[2] = mat(a->u, a->m, a->n, a->ldu, false);
     if (mat.rc) return mat.rc;
-    if (a->m == 0) { if (need) *need = 0; return DLF_OK; }
+    if (need) *need = 0;
+    if (a->m == 0) return DLF_OK;
+    if (dense_gemv_takes(a->m)) return need ? DLF_OK : launch_dense_gemv(g, s);
     Carver carve{static_cast<unsigned char*>(ws)};
     Operands op{carve};
     g.a[0] = op(g.a[0], a->m, a->k);

@@ -56,6 +56,9 @@ bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c);
 int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s);
 int dense_lat_status(cudaStream_t s, int* code);
 
+bool dense_gemv_takes(int64_t m);                             // dense_gemv.cu: forward products of a few tokens, any rows
+int launch_dense_gemv(const DenseGemm& g, cudaStream_t s);
+
 int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to, cudaStream_t s);
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s);
 

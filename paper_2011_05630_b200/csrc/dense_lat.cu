@@ -334,9 +334,9 @@ int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s
     if (!lay_out(g, c, &p, &smem)) return DLF_E_UNSUPPORTED;
     int rc = DLF_OK;
     for (int i = 0; i < 2 && rc == DLF_OK; i++) {
-        const Mat &a = g.a[i].p ? g.a[i] : g.a[0], &b = g.b[i].p ? g.b[i] : g.b[0];
-        rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, p.a_bytes / 128, 64);
-        if (rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, g.gated ? c.bn / 2 : c.bn, 64);
+        const Mat &a = g.a[i], &b = g.b[i];
+        if (a.p) rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, p.a_bytes / 128, 64);
+        if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, g.gated ? c.bn / 2 : c.bn, 64);
     }
     if (rc) return rc;
     for (int i = 0; i < 3; i++) {

@@ -23,13 +23,22 @@ __device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.0f, 1.
 constexpr float kGeluC = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGeluA = 0.044715f;
 
+// The normal distribution's density at v and its integral up to v: erfc by the rational approximation 7.1.26 of Abramowitz and Stegun,
+// "Handbook of Mathematical Functions" (off by at most 1.5e-7, half of that here), which shares its exponential with the density
+// and takes a third of the instructions of erff.
+__device__ __forceinline__ float2 normal_f(float v) {
+    const float a = fabsf(v) * 0.7071067811865476f, e = __expf(-0.5f * v * v), t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f));
+    const float tail = 0.5f * e * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f));
+    return make_float2(e * 0.3989422804014327f, v < 0.0f ? tail : 1.0f - tail);
+}
+
 // act(v).  GELU by tanh: v (1 + tanh(t)) / 2 = v sigmoid(2 t) with t = c (v + a v^3).  A NaN is 0 behind ReLU and ReLU6, as in the
 // other kernels.
 template <int ACT>
 __device__ __forceinline__ float act_f(float v) {
     if (ACT == DLF_ACT_RELU) return fmaxf(v, 0.0f);
     if (ACT == DLF_ACT_RELU6) return fminf(fmaxf(v, 0.0f), 6.0f);
-    if (ACT == DLF_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.7071067811865476f));
+    if (ACT == DLF_ACT_GELU) return v * normal_f(v).y;
     if (ACT == DLF_ACT_GELU_TANH) return v * sigmoid_f(2.0f * kGeluC * (v + kGeluA * v * v * v));
     if (ACT == DLF_ACT_SILU) return v * sigmoid_f(v);
     return v;
@@ -40,8 +49,8 @@ __device__ __forceinline__ float2 act_grad_f(float v) {
     if (ACT == DLF_ACT_RELU) return make_float2(fmaxf(v, 0.0f), v > 0.0f ? 1.0f : 0.0f);
     if (ACT == DLF_ACT_RELU6) return make_float2(fminf(fmaxf(v, 0.0f), 6.0f), v > 0.0f && v < 6.0f ? 1.0f : 0.0f);
     if (ACT == DLF_ACT_GELU) {
-        const float cdf = 0.5f * (1.0f + erff(v * 0.7071067811865476f));
-        return make_float2(v * cdf, cdf + v * __expf(-0.5f * v * v) * 0.3989422804014327f);
+        const float2 n = normal_f(v);
+        return make_float2(v * n.y, fmaf(v, n.x, n.y));
     }
     if (ACT == DLF_ACT_GELU_TANH) {
         const float s = sigmoid_f(2.0f * kGeluC * (v + kGeluA * v * v * v));

@@ -278,9 +278,9 @@ int launch_dense_pair(const DenseGemm& g, cudaStream_t s) {
     // (a tile of half the width takes 0.9 of the time: its 24 KB per 64 of K come no faster)
     if (!g.gated && (count(256) + sms / 2 - 1) / (sms / 2) * 10 > (count(128) + sms / 2 - 1) / (sms / 2) * 9) bn = 128;
     for (int i = 0; i < 2 && rc == DLF_OK; i++) {
-        const Mat &a = g.a[i].p ? g.a[i] : g.a[0], &b = g.b[i].p ? g.b[i] : g.b[0];
-        rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, 128, 64);
-        if (rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, bn / 2, 64);
+        const Mat &a = g.a[i], &b = g.b[i];
+        if (a.p) rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, 128, 64);
+        if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, bn / 2, 64);
     }
     for (int i = 0; i < 3 && rc == DLF_OK; i++) {
         p.o[i] = g.out[i];

@@ -20,34 +20,36 @@ import torch
 from . import binding as B
 
 _DTYPES = {torch.float16: B.DTYPES["f16"], torch.bfloat16: B.DTYPES["bf16"]}
-_LINEAR = struct.Struct("@ii3q6P5q")
+_LINEAR = struct.Struct("@ii3q6P5q")          # the argument structs of include/dlfusion.h
 _LINEAR_GRAD = struct.Struct("@ii3q8P7q")
 _GATED = struct.Struct("@ii3q8P6q")
 _GATED_GRAD = struct.Struct("@ii3q11P9q")
+_ops = {}   # name -> (call, its workspace query)
 
 
 def _enter(x, act):
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("a CUDA tensor is required: there is no CPU path")
-    if x.dtype not in _DTYPES:
+    dtype, a = _DTYPES.get(x.dtype), B.DENSE_ACTS.get(act)
+    if dtype is None:
         raise ValueError("float16 or bfloat16 is required, got %s" % x.dtype)
-    if act not in B.DENSE_ACTS:
+    if a is None:
         raise ValueError("act is one of %s, got %r" % (", ".join(B.DENSE_ACTS), act))
     if x.dim() != 2:
         raise ValueError("matrices have two dimensions, got %d" % x.dim())
-    return _DTYPES[x.dtype], B.DENSE_ACTS[act]
+    return dtype, a
 
 
-def _mat(t, name, rows, cols, like):
+def _mat(t, name, shape, like):
     """(pointer, row length) of a matrix, or what is wrong with it."""
     if t is None:
         return 0, 0
-    if t.dtype is not like.dtype or t.device != like.device:
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise ValueError("%s: %s on %s is required, got %s on %s" % (name, like.dtype, like.device, t.dtype, t.device))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError("%s: shape (%d, %d) is required, got %s" % (name, rows, cols, tuple(t.shape)))
+    if t.shape != shape:
+        raise ValueError("%s: shape %s is required, got %s" % (name, shape, tuple(t.shape)))
     ld, step = t.stride()
-    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+    if (step != 1 and shape[1] > 1) or (ld < shape[1] and shape[0] > 1):
         raise ValueError("%s: the values of a row have to lie side by side and rows must not overlap (strides %s)" % (name, t.stride()))
     return t.data_ptr(), ld
 
@@ -55,22 +57,27 @@ def _mat(t, name, rows, cols, like):
 def _vec(t, name, n, like):
     if t is None:
         return 0
-    if t.dtype is not torch.float32 or t.device != like.device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not torch.float32 or t.get_device() != like.get_device() or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s: %d float32 values side by side on %s are required" % (name, n, like.device))
     return t.data_ptr()
 
 
-def _call(op, args, device, ask):
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _call(op, args, device, ask)
-    lib, stream = B.lib(), torch.cuda.current_stream(device).cuda_stream
-    status = B.E_WORKSPACE if ask else getattr(lib, op)(args, None, 0, stream)
+def _call(op, args, like, ask):
+    """Enqueues on the current stream of the tensors' device, with a workspace if the call wants one (`ask`: it mostly does)."""
+    index = like.get_device()
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _call(op, args, like, ask)
+    fns = _ops.get(op)
+    if fns is None:
+        fns = _ops[op] = getattr(B.lib(), op), getattr(B.lib(), op + "_workspace_bytes")
+    stream = torch._C._cuda_getCurrentRawStream(index)   # (torch.cuda.current_stream(index).cuda_stream, 2 us faster)
+    status = B.E_WORKSPACE if ask else fns[0](args, None, 0, stream)
     if status == B.E_WORKSPACE:   # (nothing was enqueued)
         need = C.c_size_t()
-        B._check(getattr(lib, op + "_workspace_bytes")(args, C.byref(need)), op)
-        ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
-        status = getattr(lib, op)(args, ws.data_ptr() if need.value else None, need.value, stream)
+        B._check(fns[1](args, C.byref(need)), op)
+        ws = like.new_empty(need.value, dtype=torch.uint8) if need.value else None
+        status = fns[0](args, ws.data_ptr() if need.value else None, need.value, stream)
     if status != B.OK:
         raise B.DlfError(status, op)
 
@@ -81,24 +88,20 @@ def synchronize(device=None):
         B._check(B.lib().dlf_dense_sync(torch.cuda.current_stream().cuda_stream), "dlf_dense_sync")
 
 
-def _out(out, name, rows, cols, like):
-    return torch.empty((rows, cols), dtype=like.dtype, device=like.device) if out is None else out
-
-
 def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
     """y = act(x w^T + bias + residual) for x [m][k], w [n][k], residual [m][n]; with `save` (y, z), z being the sum that the
     activation was applied to.  `out` receives y and may be the residual itself."""
     dtype, a = _enter(x, act)
     m, k = x.shape
     n = w.shape[0]
-    xp, ldx = _mat(x, "x", m, k, x)
-    wp, ldw = _mat(w, "w", n, k, x)
-    rp, ldr = _mat(residual, "residual", m, n, x)
-    y = _out(out, "out", m, n, x)
-    yp, ldy = _mat(y, "out", m, n, x)
-    z = torch.empty((m, n), dtype=x.dtype, device=x.device) if save else None
+    xp, ldx = _mat(x, "x", (m, k), x)
+    wp, ldw = _mat(w, "w", (n, k), x)
+    rp, ldr = _mat(residual, "residual", (m, n), x)
+    y = x.new_empty((m, n)) if out is None else out
+    yp, ldy = (y.data_ptr(), n) if out is None else _mat(y, "out", (m, n), x)
+    z = x.new_empty((m, n)) if save else None
     _call("dlf_linear", _LINEAR.pack(dtype, a, m, k, n, xp, wp, _vec(bias, "bias", n, x), rp, yp, z.data_ptr() if save else 0,
-                                     ldx, ldw, ldr, ldy, n), x.device, False)
+                                     ldx, ldw, ldr, ldy, n), x, False)
     return (y, z) if save else y
 
 
@@ -107,22 +110,22 @@ def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, nee
     kept, needed with an activation.  dr, the residual's gradient, is dy itself where there is no activation."""
     dtype, a = _enter(dy, act)
     m, n = dy.shape
-    k = x.shape[1] if x is not None else w.shape[1]
+    k = x.shape[1] if x is not None else w.shape[1] if w is not None else 1
     if a and z is None:
         raise ValueError("z: the sum that the forward call kept is required with an activation")
     if (need_dw and x is None) or (need_dx and w is None):
         raise ValueError("x is required for dw, w for dx")
-    dyp, lddy = _mat(dy, "dy", m, n, dy)
-    xp, ldx = _mat(x, "x", m, k, dy)
-    wp, ldw = _mat(w, "w", n, k, dy)
-    zp, ldz = _mat(z, "z", m, n, dy) if a else (0, 0)
-    dx = torch.empty((m, k), dtype=dy.dtype, device=dy.device) if need_dx else None
-    dw = torch.empty((n, k), dtype=dy.dtype, device=dy.device) if need_dw else None
-    db = torch.empty((n,), dtype=torch.float32, device=dy.device) if bias else None
-    dr = torch.empty((m, n), dtype=dy.dtype, device=dy.device) if residual and a else None
+    dyp, lddy = _mat(dy, "dy", (m, n), dy)
+    xp, ldx = _mat(x, "x", (m, k), dy)
+    wp, ldw = _mat(w, "w", (n, k), dy)
+    zp, ldz = _mat(z, "z", (m, n), dy) if a else (0, 0)
+    dx = dy.new_empty((m, k)) if need_dx else None
+    dw = dy.new_empty((n, k)) if need_dw else None
+    db = dy.new_empty((n,), dtype=torch.float32) if bias else None
+    dr = dy.new_empty((m, n)) if residual and a else None
     ptr = lambda t: 0 if t is None else t.data_ptr()
     _call("dlf_linear_grad", _LINEAR_GRAD.pack(dtype, a, m, k, n, dyp, xp, wp, zp, ptr(dx), ptr(dw), ptr(db), ptr(dr),
-                                               lddy, ldx, ldw, ldz, k, k, n), dy.device, True)
+                                               lddy, ldx, ldw, ldz, k, k, n), dy, True)
     return dx, dw, db, dy if residual and not a else dr
 
 
@@ -131,15 +134,15 @@ def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
     dtype, a = _enter(x, act)
     m, k = x.shape
     n = wg.shape[0]
-    xp, ldx = _mat(x, "x", m, k, x)
-    gp, ldwg = _mat(wg, "wg", n, k, x)
-    up, ldwu = _mat(wu, "wu", n, k, x)
-    h = _out(out, "out", m, n, x)
-    hp, ldh = _mat(h, "out", m, n, x)
-    g = torch.empty((m, n), dtype=x.dtype, device=x.device) if save else None
-    u = torch.empty((m, n), dtype=x.dtype, device=x.device) if save else None
+    xp, ldx = _mat(x, "x", (m, k), x)
+    gp, ldwg = _mat(wg, "wg", (n, k), x)
+    up, ldwu = _mat(wu, "wu", (n, k), x)
+    h = x.new_empty((m, n)) if out is None else out
+    hp, ldh = (h.data_ptr(), n) if out is None else _mat(h, "out", (m, n), x)
+    g = x.new_empty((m, n)) if save else None
+    u = x.new_empty((m, n)) if save else None
     _call("dlf_gated", _GATED.pack(dtype, a, m, k, n, xp, gp, up, _vec(bg, "bg", n, x), _vec(bu, "bu", n, x), hp,
-                                   g.data_ptr() if save else 0, u.data_ptr() if save else 0, ldx, ldwg, ldwu, ldh, n, n), x.device, False)
+                                   g.data_ptr() if save else 0, u.data_ptr() if save else 0, ldx, ldwg, ldwu, ldh, n, n), x, False)
     return (h, g, u) if save else h
 
 
@@ -148,20 +151,20 @@ def gated_backward(dh, x, wg, wu, g, u, act="silu", bias=False, need_dx=True, ne
     `gated(..., save=True)` kept."""
     dtype, a = _enter(dh, act)
     m, n = dh.shape
-    k = x.shape[1] if x is not None else wg.shape[1]
+    k = x.shape[1] if x is not None else wg.shape[1] if wg is not None else 1
     if (need_dw and x is None) or (need_dx and (wg is None or wu is None)) or g is None or u is None:
         raise ValueError("g and u are required, x for the weights' gradients, wg and wu for dx")
-    dhp, lddh = _mat(dh, "dh", m, n, dh)
-    xp, ldx = _mat(x, "x", m, k, dh)
-    wgp, ldwg = _mat(wg, "wg", n, k, dh)
-    wup, ldwu = _mat(wu, "wu", n, k, dh)
-    gp, ldg = _mat(g, "g", m, n, dh)
-    up, ldu = _mat(u, "u", m, n, dh)
-    new = lambda rows: torch.empty((rows, k), dtype=dh.dtype, device=dh.device)
+    dhp, lddh = _mat(dh, "dh", (m, n), dh)
+    xp, ldx = _mat(x, "x", (m, k), dh)
+    wgp, ldwg = _mat(wg, "wg", (n, k), dh)
+    wup, ldwu = _mat(wu, "wu", (n, k), dh)
+    gp, ldg = _mat(g, "g", (m, n), dh)
+    up, ldu = _mat(u, "u", (m, n), dh)
+    new = lambda rows: dh.new_empty((rows, k))
     dx = new(m) if need_dx else None
     dwg, dwu = (new(n), new(n)) if need_dw else (None, None)
-    dbg, dbu = (torch.empty((n,), dtype=torch.float32, device=dh.device) for _ in range(2)) if bias else (None, None)
+    dbg, dbu = (dh.new_empty((n,), dtype=torch.float32) for _ in range(2)) if bias else (None, None)
     ptr = lambda t: 0 if t is None else t.data_ptr()
     _call("dlf_gated_grad", _GATED_GRAD.pack(dtype, a, m, k, n, dhp, xp, wgp, wup, gp, up, ptr(dx), ptr(dwg), ptr(dwu), ptr(dbg),
-                                             ptr(dbu), lddh, ldx, ldwg, ldwu, ldg, ldu, k, k, k), dh.device, True)
+                                             ptr(dbu), lddh, ldx, ldwg, ldwu, ldg, ldu, k, k, k), dh, True)
     return dx, dwg, dwu, dbg, dbu
