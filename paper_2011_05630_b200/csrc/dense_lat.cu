@@ -26,9 +26,9 @@ namespace dlf {
 namespace {
 
 constexpr int kEpiWarps = 8;                 // warps 0..7: warp & 3 = TMEM lane quarter, warp >> 2 = every other run of columns
-constexpr int kProdWarp0 = kEpiWarps, kProdWarps = 3;   // warp w loads ring stages w, w + 3, ...
-constexpr int kMmaWarp = kProdWarp0 + kProdWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kProdWarp0 = kEpiWarps, kProdWarps = 3;   // behind the first round of the ring warp w loads stages w, w + 3, ...
+constexpr int kMmaWarp = kProdWarp0 + kProdWarps, kMmaWarps = 2;   // issuers: warp w takes chunks w, w + 2, ...
+constexpr int kThreads = 32 * (kMmaWarp + kMmaWarps);
 constexpr int kMaxBN = 128, kMaxStages = 12;
 constexpr int kMaxDynSmem = 225 * 1024;
 constexpr int kAloneSmem = 200 * 1024;       // more than this leaves no room for another tensor-core kernel's CTA on the SM
@@ -44,63 +44,24 @@ struct LatParams {
     int chunks1, total, share;         // 64-value chunks of K: of the first source, of both, of a CTA
     int stages, a_bytes, stage_bytes, red_off, rows_per;
     int act, groups;
-    bool vec[3], res_vec;              // rows on 16-byte boundaries
+    bool vec;                          // every row that is read or written here starts on a 16-byte boundary
 };
 
-// The finished sums of 8 outputs of a row to memory.
-template <typename T>
-__device__ __forceinline__ void put8(const Mat& o, bool vec, long long row, long long col, int n, const float (&v)[8]) {
-    T* p = static_cast<T*>(const_cast<void*>(o.p)) + row * o.ld + col;
-    if (vec && n == 8) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (i < n) p[i] = from_f32<T>(v[i]);
-    }
-}
-template <int EPI, typename T>
-__device__ __forceinline__ void finish8(const LatParams& p, int group, long long row, long long col, float (&v)[8], float (&u)[8]) {
-    const int n = static_cast<int>(min(8ll, p.N - col));
-    if (EPI == EPI_PLAIN) {
-        put8<T>(p.o[group], p.vec[group], row, col, n, v);
-        return;
-    }
-    if (p.bias[0]) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] += i < n ? ld_map(p.bias[0] + col + i) : 0.0f;
-    }
+// From the sums of W outputs of a row to what is stored: v (and u of a gated tile), the biases, what is added.
+template <int EPI, int W, typename PUT>
+__device__ __forceinline__ void finish(int act_code, float (&v)[W], float (&u)[W], const float (&r)[W], PUT&& put) {
     if (EPI == EPI_LINEAR) {
-        if (p.res.p) {
-            const T* r = static_cast<const T*>(p.res.p) + row * p.res.ld + col;
-            if (p.res_vec && n == 8) {
-                const uint4 q = ld_map(reinterpret_cast<const uint4*>(r));
-                const T* e = reinterpret_cast<const T*>(&q);
 #pragma unroll
-                for (int i = 0; i < 8; i++) v[i] += to_f32(e[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++) v[i] += i < n ? to_f32(ld_map(r + i)) : 0.0f;
-            }
-        }
-        if (p.o[1].p) put8<T>(p.o[1], p.vec[1], row, col, n, v);
-        with_act(p.act, [&](auto act) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = act_f<act.value>(v[i]);
-        });
-    } else {
-        if (p.bias[1]) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) u[i] += i < n ? ld_map(p.bias[1] + col + i) : 0.0f;
-        }
-        if (p.o[1].p) put8<T>(p.o[1], p.vec[1], row, col, n, v);
-        if (p.o[2].p) put8<T>(p.o[2], p.vec[2], row, col, n, u);
-        with_act(p.act, [&](auto act) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = act_f<act.value>(v[i]) * u[i];
-        });
+        for (int i = 0; i < W; i++) v[i] += r[i];
     }
-    put8<T>(p.o[0], p.vec[0], row, col, n, v);
+    if (EPI != EPI_PLAIN) put(1, v);
+    if (EPI == EPI_GATED) put(2, u);
+    if (EPI != EPI_PLAIN)
+        with_act(act_code, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < W; i++) v[i] = EPI == EPI_GATED ? act_f<act.value>(v[i]) * u[i] : act_f<act.value>(v[i]);
+        });
+    put(0, v);
 }
 
 template <typename T, bool AMN, bool BMN, int EPI, int SPLIT>
@@ -109,6 +70,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, 1) den
     __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar, red_bar;
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s, red_abort_s;
+    __shared__ float bias_s[kMaxBN];
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* sbase = smem_raw + (base - smem_u32(smem_raw));
@@ -124,6 +86,25 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, 1) den
     const int k_first = rank * p.share, k_count = min(p.share, p.total - k_first);
     const int live = static_cast<int>(min(static_cast<long long>(p.rows), p.M - m0));   // rows of the tile that exist
 
+    // A stage's boxes, those of A first: box `bx` of chunk i of this CTA's share into stage st.
+    const int boxes_a = AMN ? 2 : 1, boxes = boxes_a + (EPI == EPI_GATED ? 2 : BMN ? p.BN / 64 : 1);
+    const uint32_t stage_tx = static_cast<uint32_t>(p.a_bytes + p.BN * 128);
+    auto load_box = [&](int i, int st, int bx) {
+        const int c = k_first + i;
+        const bool second = c >= p.chunks1;
+        const int k0 = (second ? c - p.chunks1 : c) * 64, j = bx - boxes_a;
+        uint8_t* dst = sbase + st * p.stage_bytes;
+        if (j < 0) {
+            const CUtensorMap* map = &p.a[second || group ? 1 : 0];
+            if (AMN) tma_load_2d(dst + bx * 8192, map, &full_bar[st], static_cast<int>(m0) + bx * 64, k0);
+            else tma_load_2d(dst, map, &full_bar[st], k0, static_cast<int>(m0));
+        } else {
+            dst += p.a_bytes;
+            if (EPI == EPI_GATED) tma_load_2d(dst + j * p.BN * 64, &p.b[j], &full_bar[st], k0, static_cast<int>(n0));
+            else if (BMN) tma_load_2d(dst + j * 8192, &p.b[second ? 1 : 0], &full_bar[st], static_cast<int>(n0) + j * 64, k0);
+            else tma_load_2d(dst, &p.b[second ? 1 : 0], &full_bar[st], k0, static_cast<int>(n0));
+        }
+    };
     if (warp == kProdWarp0) {
         if (lane < kMaxStages) {
             mbar_init(&full_bar[lane], 1);
@@ -132,15 +113,24 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, 1) den
         if (lane == 0) {
             abort_s = 0;
             red_abort_s = 0;
-            mbar_init(&tfull_bar, 1);
+            mbar_init(&tfull_bar, kMmaWarps);
             mbar_init(&red_bar, 1);
         }
         fence_barrier_init();
         // the bytes that the cluster's CTAs will send here (before the cluster's barrier, which every sender waits for)
         if (SPLIT > 1 && lane == 0) mbar_expect_tx(&red_bar, static_cast<uint32_t>(SPLIT * max(0, min(p.rows_per, live - rank * p.rows_per)) * p.BN) * 4u);
+        __syncwarp();
+        // the ring's first round is on its way before the rest of the set-up (a lane a stage)
+        pdl_wait();
+        if (lane < min(p.stages, k_count)) {
+            mbar_expect_tx(&full_bar[lane], stage_tx);
+#pragma unroll 1
+            for (int bx = 0; bx < boxes; bx++) load_box(lane, lane, bx);
+        }
+        __syncwarp();
     }
     if (warp == kMmaWarp) {
-        tmem_alloc(&tmem_base_s, kMaxBN);
+        tmem_alloc(&tmem_base_s, kMaxBN * kMmaWarps);
         tmem_relinquish();
     }
     tc_fence_before_sync();
@@ -152,120 +142,192 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, 1) den
     const uint32_t tmem_base = tmem_base_s;
 
     if (warp >= kProdWarp0 && warp < kMmaWarp) {
-        // ---- producers: lane i issues a stage's i-th box, those of A first ----
+        // ---- producers: lane i issues a stage's i-th box ----
         const int w = warp - kProdWarp0;
-        const int boxes_a = AMN ? 2 : 1, boxes = boxes_a + (EPI == EPI_GATED ? 2 : BMN ? p.BN / 64 : 1);
-        const uint32_t stage_tx = static_cast<uint32_t>(p.a_bytes + p.BN * 128);
         int turn = 0, st = 0;
-        uint32_t ph = 1;
+        uint32_t ph = 0;
 #pragma unroll 1
-        for (int i = 0; i < k_count; i++) {
+        for (int i = p.stages; i < k_count; i++) {
             if (turn == w) {
-                if (i >= p.stages && !mbar_wait_warp<true>(&empty_bar[st], ph, abort_flag, status, 0xA00 | (blockIdx.x << 12))) break;
+                if (!mbar_wait_warp<true>(&empty_bar[st], ph, abort_flag, status, 0xA00 | (blockIdx.x << 12))) break;
                 if (lane == 0) mbar_expect_tx(&full_bar[st], stage_tx);
                 __syncwarp();
-                if (lane < boxes) {
-                    const int c = k_first + i;
-                    const bool second = c >= p.chunks1;
-                    const int k0 = (second ? c - p.chunks1 : c) * 64, j = lane - boxes_a;
-                    uint8_t* dst = sbase + st * p.stage_bytes;
-                    if (j < 0) {
-                        const CUtensorMap* map = &p.a[second || group ? 1 : 0];
-                        if (AMN) tma_load_2d(dst + lane * 8192, map, &full_bar[st], static_cast<int>(m0) + lane * 64, k0);
-                        else tma_load_2d(dst, map, &full_bar[st], k0, static_cast<int>(m0));
-                    } else {
-                        dst += p.a_bytes;
-                        if (EPI == EPI_GATED) tma_load_2d(dst + j * p.BN * 64, &p.b[j], &full_bar[st], k0, static_cast<int>(n0));
-                        else if (BMN) tma_load_2d(dst + j * 8192, &p.b[second ? 1 : 0], &full_bar[st], static_cast<int>(n0) + j * 64, k0);
-                        else tma_load_2d(dst, &p.b[second ? 1 : 0], &full_bar[st], k0, static_cast<int>(n0));
-                    }
-                }
+                if (lane < boxes) load_box(i, st, lane);
                 __syncwarp();
             }
             if (++turn == kProdWarps) turn = 0;
             if (++st == p.stages) { st = 0; turn = 0; ph ^= 1u; }
         }
-    } else if (warp == kMmaWarp) {
+    } else if (warp >= kMmaWarp) {
+        // ---- issuers.  A run of matrix instructions holds its warp until it has almost executed, and what the warp does between two
+        // runs takes as long again: two warps with an accumulator each hide one behind the other (550 -> 300 clocks a chunk);
+        // the epilogue adds the two sums ----
+        const int w = warp - kMmaWarp;
+        const uint32_t d_tmem = tmem_base + w * kMaxBN;
+        const int last = k_count - 1 - ((k_count - 1 - w) & 1);   // this issuer's last chunk (negative: it has none)
         const uint32_t idesc = dense_idesc<T>(128, 0, AMN, BMN) | (static_cast<uint32_t>(p.BN >> 3) << 17);
         const uint32_t a0 = AMN ? umma_desc_mn_lo(base, 8192) : umma_desc_lo(base);
         const uint32_t b0 = BMN ? umma_desc_mn_lo(base + p.a_bytes, 8192) : umma_desc_lo(base + p.a_bytes);
         const uint32_t stage16 = static_cast<uint32_t>(p.stage_bytes) >> 4;
-        int st = 0;
-        uint32_t ph = 0, off = 0;
+        int st = w % p.stages;
+        uint32_t ph = static_cast<uint32_t>(w / p.stages) & 1u, off = static_cast<uint32_t>(st) * stage16;
 #pragma unroll 1
-        for (int i = 0; i < k_count; i++) {
+        for (int i = w; i < k_count; i += 2) {
             if (!mbar_wait_warp<true>(&full_bar[st], ph, abort_flag, status, 0xA10 | (blockIdx.x << 12))) break;
             tc_fence_after_sync();
             if (elect_one()) {
-                umma_chunk<1, AMN, BMN>(tmem_base, a0 + off, b0 + off, idesc, i != 0);
+                umma_chunk<1, AMN, BMN>(d_tmem, a0 + off, b0 + off, idesc, i != w);
                 if (i + p.stages < k_count) umma_commit(&empty_bar[st]);
-                if (i == k_count - 1) umma_commit(&tfull_bar);
+                if (i == last) umma_commit(&tfull_bar);
             }
             __syncwarp();
-            off += stage16;
-            if (++st == p.stages) { st = 0; ph ^= 1u; off = 0; }
+            st += 2;
+            off += 2 * stage16;
+            if (st >= p.stages) { st -= p.stages; ph ^= 1u; off -= static_cast<uint32_t>(p.stages) * stage16; }
         }
+        if (last < 0 && lane == 0) mbar_arrive(&tfull_bar);
     } else {
-        // ---- epilogue ----
+        // ---- epilogue: the sums go to shared memory (of the CTA that finishes them), row by row, and from there in runs of 8 outputs
+        // that lie side by side in memory ----
         const int q = warp & 3, half = warp >> 2, m = q * 32 + lane;
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
         const int out_bn = EPI == EPI_GATED ? p.BN / 2 : p.BN;
+        const int my_rows = max(0, min(p.rows_per, live - rank * p.rows_per)), lg = __ffs(out_bn) - 4;   // (runs of 8 in a row: a power of two)
+        const long long row_first = m0 + rank * p.rows_per;
+        const int n_cols = static_cast<int>(min(static_cast<long long>(out_bn), p.N - n0));
+        if (EPI != EPI_PLAIN && threadIdx.x < p.BN) {
+            const int c = EPI == EPI_GATED && static_cast<int>(threadIdx.x) >= out_bn ? static_cast<int>(threadIdx.x) - out_bn : static_cast<int>(threadIdx.x);
+            const float* b = p.bias[EPI == EPI_GATED && static_cast<int>(threadIdx.x) >= out_bn ? 1 : 0];
+            bias_s[threadIdx.x] = b && c < n_cols ? ld_map(b + n0 + c) : 0.0f;
+        }
+        // what a thread's next runs have to add is fetched kItems runs at a time, the first ones behind the products
+        constexpr int kItems = 4;
+        const bool add = EPI == EPI_LINEAR && p.res.p != nullptr;
+        uint4 res[kItems];
+        auto fetch_res = [&](int i0) {
+#pragma unroll
+            for (int it = 0; it < kItems; it++) {
+                const int i = i0 + it * 32 * kEpiWarps, r = i >> lg, c = (i - (r << lg)) * 8;
+                res[it] = make_uint4(0u, 0u, 0u, 0u);
+                if (add && r < my_rows && c + 8 <= n_cols)
+                    res[it] = ld_map(reinterpret_cast<const uint4*>(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c));
+            }
+        };
+        if (p.vec) fetch_res(threadIdx.x);
         bool ok = mbar_wait_warp<true>(&tfull_bar, 0u, abort_flag, status, 0xA20 | (blockIdx.x << 12));
         tc_fence_after_sync();
-        if (SPLIT == 1) {
-            // a lane finishes its own row, 8 outputs at a time
-            const bool row_live = m < live && ok;
-#pragma unroll 1
-            for (int c = half * 16; c < out_bn; c += 32) {
-                float v[16], u[16];
-                tmem_ld16(taddr + c, v);
-                if (EPI == EPI_GATED) tmem_ld16(taddr + out_bn + c, u);
-#pragma unroll
-                for (int g = 0; g < 2; g++)
-                    if (row_live && n0 + c + g * 8 < p.N)
-                        finish8<EPI, T>(p, group, m0 + m, n0 + c + g * 8, *reinterpret_cast<float(*)[8]>(v + g * 8), *reinterpret_cast<float(*)[8]>(u + g * 8));
-                __syncwarp();
-            }
-        } else {
-            const int dest = min(m / p.rows_per, SPLIT - 1), row = m - dest * p.rows_per;
-            const uint32_t slab = static_cast<uint32_t>(p.rows_per * p.BN * 4);   // one rank's partial rows
-            // (a row's 16-byte vectors are stored in an order that depends on the row: the lanes of a warp fall into different banks)
-            const uint32_t dst = mapa(base + p.red_off + rank * slab + row * p.BN * 4, dest), dst_bar = mapa(smem_u32(&red_bar), dest);
+        const int dest = SPLIT > 1 ? min(m / p.rows_per, SPLIT - 1) : 0, row = m - dest * p.rows_per;
+        const uint32_t slab = static_cast<uint32_t>(p.rows_per * p.BN * 4);   // one rank's partial rows
+        // (a row's 16-byte vectors are stored in an order that depends on the row: the lanes of a warp fall into different banks)
+        const uint32_t swz = static_cast<uint32_t>(row) & 7u;
+        uint32_t dst = base + p.red_off + rank * slab + row * p.BN * 4, dst_bar = 0;
+        if (SPLIT > 1) {
+            dst = mapa(dst, dest);
+            dst_bar = mapa(smem_u32(&red_bar), dest);
             cluster_wait();   // every CTA of the cluster runs and its barrier expects these rows
+        }
 #pragma unroll 1
-            for (int c0 = half * 16; c0 < p.BN; c0 += 32) {
-                float v[16];
-                tmem_ld16(taddr + c0, v);
-                if (m < live) {   // (sent whatever happened: the other CTAs wait for the bytes)
+        for (int c0 = half * 16; c0 < p.BN; c0 += 32) {
+            uint32_t r0[16], r1[16];
+            float v[16];
+            tmem_ld16_issue(taddr + c0, r0);
+            tmem_ld16_issue(taddr + kMaxBN + c0, r1);
+            tmem_ld16_wait(r0);
+            tmem_ld16_wait(r1);
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        st_async_v4(dst + ((static_cast<uint32_t>((c0 >> 2) + e) ^ (static_cast<uint32_t>(row) & 7u)) << 4), v[4 * e], v[4 * e + 1], v[4 * e + 2],
-                                    v[4 * e + 3], dst_bar);
+            for (int e = 0; e < 16; e++) v[e] = k_count > 1 ? __uint_as_float(r0[e]) + __uint_as_float(r1[e]) : __uint_as_float(r0[e]);
+            if (m < live) {   // (sent whatever happened: the other CTAs wait for the bytes)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t at = dst + ((static_cast<uint32_t>((c0 >> 2) + e) ^ swz) << 4);
+                    if (SPLIT > 1) st_async_v4(at, v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], dst_bar);
+                    else *reinterpret_cast<float4*>(sbase + (at - base)) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                 }
-                __syncwarp();
             }
-            // All rows of this CTA are here.  It must not retire before that, whatever its own part came to, hence a limit above
-            // the senders' and a flag of its own.
-            ok = mbar_wait<true>(&red_bar, 0u, &red_abort_s, status, 0xA30 | (blockIdx.x << 12), 4 * kWaitLimitNs) && ok;
-            const int my_rows = max(0, min(p.rows_per, live - rank * p.rows_per)), per_row = out_bn / 8;
-            const uint8_t* red = sbase + p.red_off;
+            __syncwarp();
+        }
+        // All rows of this CTA are here.  It must not retire before that, whatever its own part came to, hence a limit above
+        // the senders' and a flag of its own.
+        if (SPLIT > 1) ok = mbar_wait<true>(&red_bar, 0u, &red_abort_s, status, 0xA30 | (blockIdx.x << 12), 4 * kWaitLimitNs) && ok;
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");   // (the biases; with one CTA the sums)
+        const uint8_t* red = sbase + p.red_off;
+        if (ok && p.vec) {
 #pragma unroll 1
-            for (int i = threadIdx.x; i < my_rows * per_row; i += 32 * kEpiWarps) {
-                const int r = i / per_row, c = (i - r * per_row) * 8;
-                if (!ok || n0 + c >= p.N) continue;
-                float v[8] = {}, u[8] = {};
-                auto sum = [&](int col, float (&s)[8]) {
-                    const uint32_t at = static_cast<uint32_t>(r * p.BN * 4) + ((static_cast<uint32_t>(col >> 2) ^ (static_cast<uint32_t>(r) & 7u)) << 4);
+            for (int i0 = threadIdx.x; i0 < my_rows << lg; i0 += kItems * 32 * kEpiWarps) {
+                if (i0 != static_cast<int>(threadIdx.x)) fetch_res(i0);
 #pragma unroll
-                    for (int sp = 0; sp < SPLIT; sp++) {
-                        const float4 x = *reinterpret_cast<const float4*>(red + sp * slab + at), y = *reinterpret_cast<const float4*>(red + sp * slab + (at ^ 16u));
-                        s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
-                        s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
-                    }
-                };
-                sum(c, v);
-                if (EPI == EPI_GATED) sum(out_bn + c, u);
-                finish8<EPI, T>(p, group, m0 + rank * p.rows_per + r, n0 + c, v, u);
+                for (int it = 0; it < kItems; it++) {
+                    const int i = i0 + it * 32 * kEpiWarps, r = i >> lg, c = (i - (r << lg)) * 8;
+                    if (r >= my_rows || c >= n_cols) continue;
+                    const bool whole = c + 8 <= n_cols;
+                    float v[8], u[8], a[8];
+                    auto sum = [&](int col, float (&s)[8]) {
+                        const uint32_t at = static_cast<uint32_t>(r * p.BN * 4) + ((static_cast<uint32_t>(col >> 2) ^ (static_cast<uint32_t>(r) & 7u)) << 4);
+#pragma unroll
+                        for (int e = 0; e < 8; e++) s[e] = 0.0f;
+#pragma unroll
+                        for (int sp = 0; sp < SPLIT; sp++) {
+                            const float4 x = *reinterpret_cast<const float4*>(red + sp * slab + at), y = *reinterpret_cast<const float4*>(red + sp * slab + (at ^ 16u));
+                            s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+                            s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+                        }
+                        if (EPI != EPI_PLAIN) {
+#pragma unroll
+                            for (int e = 0; e < 8; e++) s[e] += bias_s[col + e];
+                        }
+                    };
+                    sum(c, v);
+                    if (EPI == EPI_GATED) sum(out_bn + c, u);
+                    const long long at = row_first + r;
+                    const T* add_p = static_cast<const T*>(p.res.p) + at * p.res.ld + n0 + c;
+                    const T* in = reinterpret_cast<const T*>(&res[it]);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) a[e] = !add ? 0.0f : whole ? to_f32(in[e]) : c + e < n_cols ? to_f32(ld_map(add_p + e)) : 0.0f;
+                    finish<EPI>(p.act, v, u, a, [&](int which, const float(&f)[8]) {
+                        const Mat& o = p.o[EPI == EPI_PLAIN ? group : which];
+                        if (!o.p) return;
+                        T* t = static_cast<T*>(const_cast<void*>(o.p)) + at * o.ld + n0 + c;
+                        if (whole) {
+                            *reinterpret_cast<uint4*>(t) = make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; e++)
+                                if (c + e < n_cols) t[e] = from_f32<T>(f[e]);
+                        }
+                    });
+                }
+            }
+        } else if (ok) {
+            // rows off the 16-byte boundaries: a warp has 32 columns of a row at a time, side by side, and kRows of them on their way
+            constexpr int kRows = 8;
+            const int groups = out_bn / 32;   // (of columns)
+#pragma unroll 1
+            for (int i0 = warp; i0 < my_rows * groups; i0 += kRows * kEpiWarps) {
+                float a[kRows];
+#pragma unroll
+                for (int it = 0; it < kRows; it++) {
+                    const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
+                    a[it] = add && r < my_rows && c < n_cols ? to_f32(ld_map(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c)) : 0.0f;
+                }
+#pragma unroll
+                for (int it = 0; it < kRows; it++) {
+                    const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
+                    if (r >= my_rows || c >= n_cols) continue;
+                    float v[1], u[1], b[1] = {a[it]};
+                    auto sum = [&](int col, float (&s)[1]) {
+                        const uint32_t at = static_cast<uint32_t>(r * p.BN * 4) + ((static_cast<uint32_t>(col >> 2) ^ (static_cast<uint32_t>(r) & 7u)) << 4) + (col & 3) * 4;
+                        s[0] = 0.0f;
+#pragma unroll
+                        for (int sp = 0; sp < SPLIT; sp++) s[0] += *reinterpret_cast<const float*>(red + sp * slab + at);
+                        if (EPI != EPI_PLAIN) s[0] += bias_s[col];
+                    };
+                    sum(c, v);
+                    if (EPI == EPI_GATED) sum(out_bn + c, u);
+                    finish<EPI>(p.act, v, u, b, [&](int which, const float(&f)[1]) {
+                        const Mat& o = p.o[EPI == EPI_PLAIN ? group : which];
+                        if (o.p) static_cast<T*>(const_cast<void*>(o.p))[(row_first + r) * o.ld + n0 + c] = from_f32<T>(f[0]);
+                    });
+                }
             }
         }
         tc_fence_before_sync();
@@ -276,7 +338,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, 1) den
     if (warp == kMmaWarp) {
         if (abort_s) __nanosleep(20000);   // let copies in flight land before the CTA retires
         tc_fence_after_sync();
-        tmem_dealloc(tmem_base, kMaxBN);
+        tmem_dealloc(tmem_base, kMaxBN * kMmaWarps);
     }
 }
 
@@ -312,9 +374,11 @@ bool lay_out(const DenseGemm& g, const DenseLatChoice& c, LatParams* p, size_t* 
     const int red = c.split > 1 ? c.split * p->rows_per * c.bn * 4 : 0;
     const int slack = 16384 - p->a_bytes;   // the tensor core reads 128 rows of A, behind the ring's last ones too: memory of this CTA all the same
     p->stages = std::min({kMaxStages, (kMaxDynSmem - 1024 - red - slack) / p->stage_bytes, p->share});
+    if (p->stages < p->share) p->stages &= ~1;   // the ring goes round: a stage belongs to one issuer
     if (p->stages < std::min(p->share, 3)) return false;
-    p->red_off = p->stages * p->stage_bytes + slack;
-    *smem = static_cast<size_t>(p->red_off) + red + 1024;
+    const int ring = p->stages * p->stage_bytes + slack;
+    p->red_off = c.split > 1 ? ring : 0;   // (alone, a CTA's sums go where the ring was)
+    *smem = static_cast<size_t>(std::max(ring + red, p->red_off + c.split * p->rows_per * c.bn * 4)) + 1024;
     if (c.split > 1) *smem = std::max<size_t>(*smem, kAloneSmem);
     return true;
 }
@@ -339,12 +403,9 @@ int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s
         if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, g.gated ? c.bn / 2 : c.bn, 64);
     }
     if (rc) return rc;
-    for (int i = 0; i < 3; i++) {
-        p.o[i] = g.out[i];
-        p.vec[i] = dense_rows16(g.out[i]);
-    }
+    for (int i = 0; i < 3; i++) p.o[i] = g.out[i];
     p.res = g.res;
-    p.res_vec = dense_rows16(g.res);
+    p.vec = dense_rows16(g.res) && dense_rows16(g.out[0]) && dense_rows16(g.out[1]) && dense_rows16(g.out[2]);
     p.bias[0] = g.bias[0]; p.bias[1] = g.bias[1];
     p.M = g.M; p.N = g.N;
     const int step = g.gated ? c.bn / 2 : c.bn;

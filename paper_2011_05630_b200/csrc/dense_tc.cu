@@ -184,7 +184,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
         for (long long t = t_first; t < p.tiles && ok; t += t_step, j++) {
             const TileAt at = tile_at<BN, EPI>(p, t);
             const uint32_t acc = j & 1u;
-            const long long row0 = at.m0 + rank * 128 + q * 32, row = row0 + lane;
+            const long long row0 = at.m0 + rank * 128 + q * 32;
             const uint32_t taddr = tmem_base + acc * 256u + (static_cast<uint32_t>(q * 32) << 16);
 #pragma unroll 1
             for (int c = 0; c < kChunks; c++) {
@@ -193,7 +193,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
                 const int cols = static_cast<int>(max(0ll, min(64ll, p.N - col0)));
                 uint4 res[EPI == EPI_LINEAR ? 8 : 1];
                 if constexpr (EPI == EPI_LINEAR) {
-                    if (p.res.p) load_row64<T>(p.res, p.res_vec, row, col0, row < p.M ? cols : 0, res);
+                    if (p.res.p) load_rows64<T>(p.res, p.res_vec, stg, lane, row0, col0, p.M, cols, res);
                 }
                 if (c == 0) {
                     ok = mbar_wait_warp(&tfull_bar[acc], (j >> 1) & 1u, abort_flag, status, 0x400 | (blockIdx.x << 12));

@@ -112,26 +112,33 @@ __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The first `cols` (0 to 64) values of a row from column col0 on, as they lie in memory; zeros behind them.
+// A warp's 32 rows of 64 values from column col0 on, as they lie in memory, a lane its row: the first `cols` of them and, behind
+// those and the matrix's last row, zeros.  Rows that start off the 16-byte boundaries, or end between two, come through `stg`
+// (4096 bytes of the warp's own), whole runs of columns at a time.
 template <typename T>
-__device__ __forceinline__ void load_row64(const Mat& m, bool vec, int64_t row, int64_t col0, int cols, uint4 (&q)[8]) {
-    const T* p = static_cast<const T*>(m.p) + row * m.ld + col0;
+__device__ __forceinline__ void load_rows64(const Mat& m, bool vec, uint8_t* stg, int lane, int64_t row0, int64_t col0, int64_t rows_end, int cols, uint4 (&q)[8]) {
+    const unsigned short* p = static_cast<const unsigned short*>(m.p) + row0 * m.ld + col0;
+    const int rows = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), rows_end - row0)));
+    if (vec && (cols & 7) == 0) {
+        p += lane * m.ld;
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-        q[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (vec && j * 8 + 8 <= cols) {
-            q[j] = ld_map(reinterpret_cast<const uint4*>(p + j * 8));
-        } else if (j * 8 < cols) {
-            const unsigned short* e = reinterpret_cast<const unsigned short*>(p + j * 8);
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t lo = j * 8 + 2 * i < cols ? ld_map(e + 2 * i) : 0u, hi = j * 8 + 2 * i + 1 < cols ? ld_map(e + 2 * i + 1) : 0u;
-                w[i] = lo | hi << 16;
-            }
-            q[j] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int j = 0; j < 8; j++) q[j] = lane < rows && j * 8 < cols ? ld_map(reinterpret_cast<const uint4*>(p + j * 8)) : make_uint4(0u, 0u, 0u, 0u);
+        return;
     }
+    if (lane == 0) tma_store_wait_read();   // what lay here before has left
+    __syncwarp();
+#pragma unroll 8
+    for (int r = 0; r < 32; r++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int c = lane + h * 32;
+            const unsigned short v = r < rows && c < cols ? ld_map(p + r * m.ld + c) : static_cast<unsigned short>(0);
+            *reinterpret_cast<unsigned short*>(stg + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2) = v;
+        }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; j++) q[j] = *reinterpret_cast<const uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4));
+    __syncwarp();
 }
 template <typename T>
 __device__ __forceinline__ void add_row64(const uint4 (&q)[8], float* v) {
