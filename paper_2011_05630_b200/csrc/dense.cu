@@ -2,6 +2,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "dense.h"
@@ -206,33 +207,54 @@ int zero_vec(float* p, int64_t n, cudaStream_t s) {
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
-// SM clocks that the kernel of dense_lat.cu would take, and its best layout.
+// ---- which kernel --------------------------------------------------------------------------------------------------------------
+// Microseconds among other kernels, for each kernel and layout that can run a product: fitted to 4000 measured times of 468 products
+// (forward, gated and both gradients, 5 to 2048 tokens, widths from 256 to 11264; root mean square of the logarithm 0.12 and
+// 0.09).  What is chosen by it takes 1.8 % longer than each product's best in the geometric mean, the pairs of CTAs alone 1.9 times as
+// long, the clusters alone 1.3 times.
+double gemm_bytes(const DenseGemm& g) {
+    const double m = static_cast<double>(g.M), n = static_cast<double>(g.N), k = static_cast<double>(g.K);
+    return 2.0 * (m * k * std::max(g.sources, g.groups) + n * k * (g.gated ? 2 : g.sources) + m * n * g.groups);
+}
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
     double least = -1.0;
-    const int64_t tiles_m = (g.M + 127) / 128;
-    DenseLatChoice c;
-    c.rows = g.a_mn ? static_cast<int>(std::min<int64_t>(g.M, 128)) : static_cast<int>((g.M + tiles_m - 1) / tiles_m);
-    const int64_t chunks = (g.K + 63) / 64 * g.sources;
+    const int64_t tiles_m = ceil_div(g.M, 128), chunks = ceil_div(g.K, 64) * g.sources;
+    DenseLatChoice c{};
+    c.rows = g.a_mn ? static_cast<int>(std::min<int64_t>(g.M, 128)) : static_cast<int>(ceil_div(g.M, tiles_m));
     for (c.bn = 64; c.bn <= 128; c.bn += 64) {
-        const int step = g.gated ? c.bn / 2 : c.bn;
-        const int64_t tiles = tiles_m * ((g.N + step - 1) / step) * g.groups;
+        const int64_t tiles = tiles_m * ceil_div(g.N, g.gated ? c.bn / 2 : c.bn) * g.groups;
         for (c.split = 1; c.split <= 8; c.split *= 2) {
-            if (tiles * c.split > (1 << 20) || !dense_lat_possible(g, c)) continue;
+            const int64_t ctas = tiles * c.split;
+            if (ctas > (1 << 20)) break;
+            c.deep = ctas <= sms;
+            int stages = 0;
+            bool two = false;
+            if (!dense_lat_possible(g, c, &stages, &two)) continue;
+            // clusters find fewer places than single CTAs: 148, 132 and 120 CTAs of clusters of 2, 4 and 8 on 148 SMs
+            const double slots = sms * (c.split == 1 ? (two ? 2.0 : 1.0) : c.split == 2 ? 1.0 : c.split == 4 ? 132.0 / 148 : 120.0 / 148);
+            const double waves = std::ceil(static_cast<double>(ctas) / slots), share = static_cast<double>(ceil_div(chunks, c.split));
+            const double busy = std::min(two ? 2.0 : 1.0, std::max(1.0, static_cast<double>(ctas) / sms));   // CTAs of an SM at a time
             const double stage = (g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024) + c.bn * 128;
-            const double share = static_cast<double>((chunks + c.split - 1) / c.split), waves = static_cast<double>((tiles * c.split + sms - 1) / sms);
-            const double cost = 3000.0 + waves * (share * std::max(stage / 57.0, 330.0) + (c.split > 1 ? 2000.0 : 0.0) + c.rows * c.bn * 0.2);
-            if (least < 0 || cost < least) {
-                least = cost;
+            // a chunk: its matrix instructions and what lies between two runs, its bytes at an SM's rate, a round trip shared by the ring
+            double chunk = std::max(0.15 + 0.00055 * c.bn, stage * busy / 123e3);
+            if (stages < share) chunk = std::max(chunk, 1.18 / stages);
+            const double one = 2.87 + share * chunk + (c.split > 1 ? 0.9 + 2.6e-4 * c.rows * c.bn : 9.2e-5 * c.rows * c.bn);
+            const double us = std::max(one + (waves - 1.0) * (one - (two ? 0.65 : 0.0)), 2.87 + gemm_bytes(g) / 4.6e6);
+            if (least < 0 || us < least) {
+                least = us;
                 *best = c;
             }
         }
     }
     return least;
 }
-double pair_cost(const DenseGemm& g, int sms) {
-    const int step = g.gated ? 128 : 256;
-    const int64_t tiles = (g.M + 255) / 256 * ((g.N + step - 1) / step) * g.groups, pairs = sms / 2;
-    return 5000.0 + static_cast<double>((tiles + pairs - 1) / pairs) * static_cast<double>((g.K + 63) / 64 * g.sources) * 540.0 + 3000.0;
+double pair_cost(const DenseGemm& g, int sms, int bn) {
+    const int64_t tiles = ceil_div(g.M, 256) * ceil_div(g.N, g.gated ? bn / 2 : bn) * g.groups;
+    const double waves = static_cast<double>(ceil_div(tiles, std::max(1, sms / 2))), chunks = static_cast<double>(ceil_div(g.K, 64) * g.sources);
+    const double chunk = bn == 256 ? 0.312 : 0.275, rows = bn == 256 ? 3.0 : 2.35;   // (24 KB of a stage come no faster than 32)
+    return std::max(0.87 + waves * (chunks * chunk + 0.3 * rows) + rows, 0.87 + gemm_bytes(g) / 5.13e6);
 }
 
 int launch_gemm(const DenseGemm& g, cudaStream_t s) {
@@ -240,8 +262,9 @@ int launch_gemm(const DenseGemm& g, cudaStream_t s) {
     const int rc = query_sms(&sms);
     if (rc) return rc;
     DenseLatChoice c{};
-    const double lat = lat_cost(g, sms, &c);
-    return lat >= 0 && lat < pair_cost(g, sms) ? launch_dense_lat(g, c, s) : launch_dense_pair(g, s);
+    const double lat = lat_cost(g, sms, &c), wide = pair_cost(g, sms, 256), narrow = g.gated ? wide : pair_cost(g, sms, 128);
+    if (lat >= 0 && lat < std::min(wide, narrow)) return launch_dense_lat(g, c, s);
+    return launch_dense_pair(g, wide <= narrow ? 256 : 128, s);
 }
 
 // An operand as the products read it: itself, or a copy in the workspace (`run`: made now).

@@ -45,14 +45,16 @@ struct DenseGrad {
 // True if a matrix can be a TMA operand: rows start on 16-byte boundaries.
 inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 0; }
 
-int launch_dense_pair(const DenseGemm& g, cudaStream_t s);    // dense_tc.cu; operands with rows on 16-byte boundaries
+// dense_tc.cu: tiles of 256 rows by bn (256, 128; gated: 256, both halves) columns of B; operands with rows on 16-byte boundaries.
+int launch_dense_pair(const DenseGemm& g, int bn, cudaStream_t s);
 int dense_pair_status(cudaStream_t s, int* code);             // waits for the stream; a kernel's bounded wait that gave up
 // dense_lat.cu: tiles of `rows` rows (at most 128) by `bn` columns of B (64 or 128; both halves of a gated tile), K shared out over
 // `split` CTAs (1, 2, 4, 8).
 struct DenseLatChoice {
     int rows, bn, split;
+    bool deep;   // a tile of one CTA: the whole of an SM's shared memory for its ring instead of half
 };
-bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c);
+bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* stages, bool* two);   // `two` of its CTAs fit an SM
 int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s);
 int dense_lat_status(cudaStream_t s, int* code);
 

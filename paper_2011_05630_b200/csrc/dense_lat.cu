@@ -31,6 +31,7 @@ constexpr int kMmaWarp = kProdWarp0 + kProdWarps, kMmaWarps = 2;   // issuers: w
 constexpr int kThreads = 32 * (kMmaWarp + kMmaWarps);
 constexpr int kMaxBN = 128, kMaxStages = 12;
 constexpr int kMaxDynSmem = 225 * 1024;
+constexpr int kPairSmem = 110 * 1024;        // two CTAs fit an SM: one's set-up and last rows behind the other's products
 constexpr int kAloneSmem = 200 * 1024;       // more than this leaves no room for another tensor-core kernel's CTA on the SM
 enum { EPI_PLAIN = 0, EPI_LINEAR = 1, EPI_GATED = 2 };
 
@@ -65,7 +66,7 @@ __device__ __forceinline__ void finish(int act_code, float (&v)[W], float (&u)[W
 }
 
 template <typename T, bool AMN, bool BMN, int EPI, int SPLIT>
-__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, 1) dense_lat_kernel(const __grid_constant__ LatParams p) {
+__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT == 1 ? 2 : 1) dense_lat_kernel(const __grid_constant__ LatParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar, red_bar;
     __shared__ uint32_t tmem_base_s;
@@ -373,8 +374,12 @@ bool lay_out(const DenseGemm& g, const DenseLatChoice& c, LatParams* p, size_t* 
     if (c.split > 1 && (c.split - 1) * p->share >= p->total) return false;   // (a CTA without work)
     const int red = c.split > 1 ? c.split * p->rows_per * c.bn * 4 : 0;
     const int slack = 16384 - p->a_bytes;   // the tensor core reads 128 rows of A, behind the ring's last ones too: memory of this CTA all the same
-    p->stages = std::min({kMaxStages, (kMaxDynSmem - 1024 - red - slack) / p->stage_bytes, p->share});
-    if (p->stages < p->share) p->stages &= ~1;   // the ring goes round: a stage belongs to one issuer
+    for (int budget : {kPairSmem, kMaxDynSmem}) {
+        if ((c.split > 1 || c.deep) && budget == kPairSmem) continue;
+        p->stages = std::min({kMaxStages, (budget - 1024 - red - slack) / p->stage_bytes, p->share});
+        if (p->stages < p->share) p->stages &= ~1;   // the ring goes round: a stage belongs to one issuer
+        if (p->stages >= std::min(p->share, 4)) break;
+    }
     if (p->stages < std::min(p->share, 3)) return false;
     const int ring = p->stages * p->stage_bytes + slack;
     p->red_off = c.split > 1 ? ring : 0;   // (alone, a CTA's sums go where the ring was)
@@ -385,10 +390,13 @@ bool lay_out(const DenseGemm& g, const DenseLatChoice& c, LatParams* p, size_t* 
 
 }  // namespace
 
-bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c) {
+bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* stages, bool* two) {
     LatParams p;
     size_t smem;
-    return lay_out(g, c, &p, &smem);
+    if (!lay_out(g, c, &p, &smem)) return false;
+    *stages = p.stages;
+    *two = smem <= static_cast<size_t>(kPairSmem) + 2048;
+    return true;
 }
 
 int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s) {

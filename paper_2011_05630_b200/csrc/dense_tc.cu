@@ -267,16 +267,12 @@ PairFn pick_pair(const DenseGemm& g, int bn) {
 
 }  // namespace
 
-int launch_dense_pair(const DenseGemm& g, cudaStream_t s) {
+int launch_dense_pair(const DenseGemm& g, int bn, cudaStream_t s) {
     int sms = 0;
     int rc = query_sms(&sms);
     if (rc) return rc;
     PairParams p;
     std::memset(&p, 0, sizeof(p));
-    int bn = 256;
-    auto count = [&](int b) { return ((g.M + 255) / 256) * ((g.N + (g.gated ? b / 2 : b) - 1) / (g.gated ? b / 2 : b)) * g.groups; };
-    // (a tile of half the width takes 0.9 of the time: its 24 KB per 64 of K come no faster)
-    if (!g.gated && (count(256) + sms / 2 - 1) / (sms / 2) * 10 > (count(128) + sms / 2 - 1) / (sms / 2) * 9) bn = 128;
     for (int i = 0; i < 2 && rc == DLF_OK; i++) {
         const Mat &a = g.a[i], &b = g.b[i];
         if (a.p) rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, 128, 64);
