@@ -20,40 +20,47 @@ namespace {
 // and walks rows, so that a column's sum stays in one thread's registers; kGradSplit CTAs share the rows of a strip as a cluster
 // and their column sums meet in distributed shared memory, added up in the order of the ranks: the same bits every time, no
 // atomics and no second kernel.
-constexpr int kGradCols = 64, kGradThreads = 256, kGradSplit = 8;
+constexpr int kGradCols = 64, kGradThreads = 128, kGradSplit = 8;
 
-// V values of a row, as they lie in memory; those behind the row's end (n of them exist) are zero and stay unwritten.
+// V values of a row, as they lie in memory: 8 on a 16-byte boundary, or 2 anywhere; `n` of them exist (of 8 all or none).
 template <typename T, int V>
-struct alignas(V * 2) Run {
-    T v[V];
-    __device__ __forceinline__ float get(int i) const { return to_f32(v[i]); }
-    __device__ __forceinline__ void set(int i, float f) { v[i] = from_f32<T>(f); }
+struct Run;
+template <typename T>
+struct Run<T, 8> {
+    uint4 q;
     __device__ __forceinline__ void load(const Mat& m, int64_t row, int64_t col, int n) {
-        const T* p = static_cast<const T*>(m.p) + row * m.ld + col;
-        if (V == 8 && n == 8) {
-            *reinterpret_cast<uint4*>(v) = ld_map(reinterpret_cast<const uint4*>(p));
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; i++) v[i] = i < n ? ld_map(p + i) : from_f32<T>(0.0f);
-        }
+        q = make_uint4(0u, 0u, 0u, 0u);
+        if (n) q = ld_map(reinterpret_cast<const uint4*>(static_cast<const T*>(m.p) + row * m.ld + col));
     }
+    __device__ __forceinline__ float2 get2(int i) const { return unpack2<T>(i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w); }
+    __device__ __forceinline__ void set2(int i, float2 f) { (i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w) = pack2<T>(f.x, f.y); }
+    __device__ __forceinline__ void store(const Mat& m, int64_t row, int64_t col, int) const {
+        if (m.p) *reinterpret_cast<uint4*>(static_cast<T*>(const_cast<void*>(m.p)) + row * m.ld + col) = q;
+    }
+};
+template <typename T>
+struct Run<T, 2> {
+    uint32_t q;
+    __device__ __forceinline__ void load(const Mat& m, int64_t row, int64_t col, int n) {
+        const unsigned short* p = static_cast<const unsigned short*>(m.p) + row * m.ld + col;
+        const uint32_t lo = n > 0 ? ld_map(p) : 0u, hi = n > 1 ? ld_map(p + 1) : 0u;
+        q = lo | hi << 16;
+    }
+    __device__ __forceinline__ float2 get2(int) const { return unpack2<T>(q); }
+    __device__ __forceinline__ void set2(int, float2 f) { q = pack2<T>(f.x, f.y); }
     __device__ __forceinline__ void store(const Mat& m, int64_t row, int64_t col, int n) const {
         if (!m.p) return;
-        T* p = static_cast<T*>(const_cast<void*>(m.p)) + row * m.ld + col;
-        if (V == 8 && n == 8) {
-            *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; i++)
-                if (i < n) p[i] = v[i];
-        }
+        unsigned short* p = static_cast<unsigned short*>(const_cast<void*>(m.p)) + row * m.ld + col;
+        p[0] = static_cast<unsigned short>(q);
+        if (n > 1) p[1] = static_cast<unsigned short>(q >> 16);
     }
 };
 
-template <typename T, int V, bool GATED>
-__global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThreads, GATED ? 2 : 3) dense_grad_kernel(const __grid_constant__ DenseGrad g) {
+template <typename T, int V, bool GATED, int ACT>
+__global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThreads, GATED ? 5 : 7) dense_grad_kernel(const __grid_constant__ DenseGrad g) {
     constexpr int TX = kGradCols / V, TY = kGradThreads / TX;
-    __shared__ float red[GATED ? 2 : 1][TY][kGradCols];
+    constexpr int kParts = V == 8 ? kGradThreads / 32 : TY;   // partial sums of a column: of a warp's four rows, or a thread's own
+    __shared__ float red[GATED ? 2 : 1][kParts][kGradCols];
     pdl_wait();
     pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
@@ -61,60 +68,91 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
     const int64_t strip = blockIdx.x / kGradSplit;
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
     const int64_t col = strip * kGradCols + tx * V;
-    const int n = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(V), g.N - col)));
-    float s0[V] = {}, s1[V] = {};
-    // rows are dealt out round by round, so that the CTAs of a strip are never far apart; kRows of a thread's rows are on their way at
-    // a time
-    constexpr int kRows = V == 8 ? 4 : 8;
+    const int n = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(V), g.N - col)));   // (with V == 8 the columns are a multiple of 8)
+    constexpr int VP = V / 2;   // pairs of values
+    float2 s0[VP] = {}, s1[VP] = {};
+    // rows are dealt out round by round, so that the CTAs of a strip are never far apart; the next kRows of a thread's rows are on their
+    // way while these are worked on
+    constexpr int kRows = V == 8 ? 2 : 4;
     constexpr int64_t kStep = static_cast<int64_t>(TY) * kGradSplit;
-    const bool with_z = GATED || g.act != DLF_ACT_NONE;
-    if (n > 0)
-#pragma unroll 1
-        for (int64_t row0 = static_cast<int64_t>(rank) * TY + ty; row0 < g.M; row0 += kRows * kStep) {
-            Run<T, V> dy[kRows], z[kRows], u[GATED ? kRows : 1];
+    Run<T, V> dy[2][kRows], z[2][kRows], u[2][GATED ? kRows : 1];
+    auto fetch = [&](int b, int64_t row0) {
 #pragma unroll
-            for (int r = 0; r < kRows; r++) {
-                const int64_t row = row0 + r * kStep;
-                if (row >= g.M) break;
-                dy[r].load(g.dy, row, col, n);
-                if (with_z) z[r].load(g.z, row, col, n);
-                if (GATED) u[GATED ? r : 0].load(g.u, row, col, n);
-            }
-            with_act(g.act, [&](auto act) {
-#pragma unroll
-                for (int r = 0; r < kRows; r++) {
-                    const int64_t row = row0 + r * kStep;
-                    if (row >= g.M) break;
-                    Run<T, V> d, e;
-#pragma unroll
-                    for (int i = 0; i < V; i++) {
-                        const float2 a = act_grad_f<act.value>(GATED || act.value != DLF_ACT_NONE ? z[r].get(i) : 0.0f);
-                        const float t = dy[r].get(i);
-                        const float v = GATED ? t * u[GATED ? r : 0].get(i) * a.y : t * a.y;
-                        s0[i] += v;
-                        d.set(i, v);
-                        if (GATED) {
-                            s1[i] += t * a.x;
-                            e.set(i, t * a.x);
-                        }
-                    }
-                    d.store(g.d0, row, col, n);
-                    if (GATED) e.store(g.d1, row, col, n);
-                    else d.store(g.d0c, row, col, n);
-                }
-            });
+        for (int r = 0; r < kRows; r++) {
+            const int64_t row = row0 + r * kStep;
+            const int here = row < g.M ? n : 0;
+            dy[b][r].load(g.dy, row, col, here);
+            if (GATED || ACT != DLF_ACT_NONE) z[b][r].load(g.z, row, col, here);
+            if (GATED) u[b][GATED ? r : 0].load(g.u, row, col, here);
         }
-    if (!g.db0 && !g.db1) return;   // (the same for every thread of the cluster)
+    };
+    auto work = [&](int b, int64_t row0) {
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        red[0][ty][tx * V + i] = s0[i];
-        if (GATED) red[GATED ? 1 : 0][ty][tx * V + i] = s1[i];
+        for (int r = 0; r < kRows; r++) {
+            const int64_t row = row0 + r * kStep;
+            if (row >= g.M) break;
+            Run<T, V> d, e;
+#pragma unroll
+            for (int i = 0; i < VP; i++) {
+                float2 value, slope;
+                const float2 t = dy[b][r].get2(i);
+                act_grad2<ACT>(GATED || ACT != DLF_ACT_NONE ? z[b][r].get2(i) : t, &value, &slope);
+                if (GATED) {
+                    const float2 q = mul2(t, value);
+                    s1[i] = add2(s1[i], q);
+                    e.set2(i, q);
+                    slope = mul2(slope, u[b][GATED ? r : 0].get2(i));
+                }
+                const float2 q = mul2(t, slope);
+                s0[i] = add2(s0[i], q);
+                d.set2(i, q);
+            }
+            d.store(g.d0, row, col, n);
+            if (GATED) e.store(g.d1, row, col, n);
+            else d.store(g.d0c, row, col, n);
+        }
+    };
+    if (n > 0) {
+        int64_t row0 = static_cast<int64_t>(rank) * TY + ty;
+        fetch(0, row0);
+#pragma unroll 1
+        while (row0 < g.M) {
+            fetch(1, row0 + kRows * kStep);
+            work(0, row0);
+            row0 += kRows * kStep;
+            if (row0 >= g.M) break;
+            fetch(0, row0 + kRows * kStep);
+            work(1, row0);
+            row0 += kRows * kStep;
+        }
+    }
+    if (!g.db0 && !g.db1) return;   // (the same for every thread of the cluster)
+    if (V == 8) {   // (a warp has four rows of the strip's eight vectors)
+        auto meet = [](float2 v) {
+#pragma unroll
+            for (int d = 8; d < 32; d <<= 1) v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, d), __shfl_xor_sync(0xffffffffu, v.y, d)));
+            return v;
+        };
+#pragma unroll
+        for (int i = 0; i < VP; i++) {
+            s0[i] = meet(s0[i]);
+            if (GATED) s1[i] = meet(s1[i]);
+        }
+    }
+    const int part = V == 8 ? static_cast<int>(threadIdx.x) / 32 : ty;
+    if (V != 8 || (threadIdx.x & 31) < TX) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            red[0][part][tx * V + i] = i & 1 ? s0[i / 2].y : s0[i / 2].x;
+            if (GATED) red[GATED ? 1 : 0][part][tx * V + i] = i & 1 ? s1[i / 2].y : s1[i / 2].x;
+        }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < (GATED ? 2 : 1) * kGradCols; i += kGradThreads) {
         const int which = i / kGradCols, c = i % kGradCols;
         float s = 0.0f;
-        for (int y = 0; y < TY; y++) s += red[which][y][c];
+#pragma unroll
+        for (int y = 0; y < kParts; y++) s += red[which][y][c];
         red[which][0][c] = s;
     }
     cluster.sync();
@@ -128,6 +166,21 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
         }
     cluster.sync();   // no CTA leaves while its sums are still read
 }
+
+typedef void (*GradFn)(const DenseGrad);
+template <typename T, int V, bool GATED>
+GradFn pick_grad_act(int act) {
+    switch (act) {
+        case DLF_ACT_RELU: return dense_grad_kernel<T, V, GATED, DLF_ACT_RELU>;
+        case DLF_ACT_RELU6: return dense_grad_kernel<T, V, GATED, DLF_ACT_RELU6>;
+        case DLF_ACT_GELU: return dense_grad_kernel<T, V, GATED, DLF_ACT_GELU>;
+        case DLF_ACT_GELU_TANH: return dense_grad_kernel<T, V, GATED, DLF_ACT_GELU_TANH>;
+        case DLF_ACT_SILU: return dense_grad_kernel<T, V, GATED, DLF_ACT_SILU>;
+        default: return dense_grad_kernel<T, V, GATED, DLF_ACT_NONE>;
+    }
+}
+template <typename T, int V>
+GradFn pick_grad(bool gated, int act) { return gated ? pick_grad_act<T, V, true>(act) : pick_grad_act<T, V, false>(act); }
 
 // ---- rows onto 16-byte boundaries --------------------------------------------------------------------------------------------
 // For an operand whose rows start anywhere: the tensor-core kernels load tiles by TMA, which takes 16-byte boundaries only.  A copy costs
@@ -210,8 +263,8 @@ int zero_vec(float* p, int64_t n, cudaStream_t s) {
 // ---- which kernel --------------------------------------------------------------------------------------------------------------
 // Microseconds among other kernels, for each kernel and layout that can run a product: fitted to 4000 measured times of 468 products
 // (forward, gated and both gradients, 5 to 2048 tokens, widths from 256 to 11264; root mean square of the logarithm 0.12 and
-// 0.09).  What is chosen by it takes 1.8 % longer than each product's best in the geometric mean, the pairs of CTAs alone 1.9 times as
-// long, the clusters alone 1.3 times.
+// 0.09).  What is chosen by it takes 1.8 % longer than each product's best in the geometric mean, the best of the pairs alone 33 %, the
+// best of the clusters alone (where they can run at all) 10 %.
 double gemm_bytes(const DenseGemm& g) {
     const double m = static_cast<double>(g.M), n = static_cast<double>(g.N), k = static_cast<double>(g.K);
     return 2.0 * (m * k * std::max(g.sources, g.groups) + n * k * (g.gated ? 2 : g.sources) + m * n * g.groups);
@@ -481,19 +534,14 @@ int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to
 
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
     auto vec = [](const Mat& m) { return !m.p || (aligned(16, m.p) && m.ld % 8 == 0); };
-    const bool v8 = vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
+    const bool v8 = g.N % 8 == 0 && vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
     const int64_t blocks = (g.N + kGradCols - 1) / kGradCols * kGradSplit;   // (at most 2^27)
     const int grid = static_cast<int>(blocks);
-    auto go = [&](auto kernel) {
-        const cudaError_t e = launch_kernel(kernel, grid, kGradThreads, 0, s, g);
-        return e == cudaSuccess ? DLF_OK : cuda_fail(e);
-    };
-    if (g.dtype == DLF_BF16) {
-        if (g.gated) return v8 ? go(dense_grad_kernel<__nv_bfloat16, 8, true>) : go(dense_grad_kernel<__nv_bfloat16, 1, true>);
-        return v8 ? go(dense_grad_kernel<__nv_bfloat16, 8, false>) : go(dense_grad_kernel<__nv_bfloat16, 1, false>);
-    }
-    if (g.gated) return v8 ? go(dense_grad_kernel<__half, 8, true>) : go(dense_grad_kernel<__half, 1, true>);
-    return v8 ? go(dense_grad_kernel<__half, 8, false>) : go(dense_grad_kernel<__half, 1, false>);
+    GradFn fn = nullptr;
+    if (g.dtype == DLF_BF16) fn = v8 ? pick_grad<__nv_bfloat16, 8>(g.gated, g.act) : pick_grad<__nv_bfloat16, 2>(g.gated, g.act);
+    else fn = v8 ? pick_grad<__half, 8>(g.gated, g.act) : pick_grad<__half, 2>(g.gated, g.act);
+    const cudaError_t e = launch_kernel(fn, grid, kGradThreads, 0, s, g);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
 }  // namespace dlf

@@ -60,7 +60,12 @@ __device__ __forceinline__ void finish(int act_code, float (&v)[W], float (&u)[W
     if (EPI != EPI_PLAIN)
         with_act(act_code, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < W; i++) v[i] = EPI == EPI_GATED ? act_f<act.value>(v[i]) * u[i] : act_f<act.value>(v[i]);
+            for (int i = 0; i + 1 < W; i += 2) {
+                float2 a = act2<act.value>(make_float2(v[i], v[i + 1]));
+                if (EPI == EPI_GATED) a = mul2(a, make_float2(u[i], u[i + 1]));
+                v[i] = a.x; v[i + 1] = a.y;
+            }
+            if (W % 2) v[W - 1] = EPI == EPI_GATED ? act_f<act.value>(v[W - 1]) * u[W - 1] : act_f<act.value>(v[W - 1]);
         });
     put(0, v);
 }

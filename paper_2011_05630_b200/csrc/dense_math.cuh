@@ -17,51 +17,135 @@ __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2hal
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// 1 / (1 + e^-v).  The quotient's denominator is above 2^126 only where the value is below 2^-126; 0 then.
-__device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.0f, 1.0f + __expf(-v)); }
+// Two values rounded, the first one in the lower half.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t v);
+template <>
+__device__ __forceinline__ float2 unpack2<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+template <>
+__device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+
+// Two values at a time: sums and products of pairs are single instructions.
+__device__ __forceinline__ unsigned long long pair_bits(float2 v) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 pair_of(unsigned long long r) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+    return v;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// 2^v and 1 / v to 2^-22, without the scaling that subnormal values would need (2^v below 2^-126 is 0, and so is 1 / v above 2^126).
+__device__ __forceinline__ float2 exp2_2(float2 v) {
+    float2 r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(v.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 rcp2(float2 v) {
+    float2 r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(v.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(v.y));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float2 sigmoid2(float2 v) { return rcp2(add2(exp2_2(mul2(v, both(-kLog2e))), both(1.0f))); }   // 1 / (1 + e^-v)
 
 constexpr float kGeluC = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGeluA = 0.044715f;
 
 // The normal distribution's density at v and its integral up to v: erfc by the rational approximation 7.1.26 of Abramowitz and Stegun,
-// "Handbook of Mathematical Functions" (off by at most 1.5e-7, half of that here), which shares its exponential with the density
-// and takes a third of the instructions of erff.
-__device__ __forceinline__ float2 normal_f(float v) {
-    const float a = fabsf(v) * 0.7071067811865476f, e = __expf(-0.5f * v * v), t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f));
-    const float tail = 0.5f * e * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f));
-    return make_float2(e * 0.3989422804014327f, v < 0.0f ? tail : 1.0f - tail);
+// "Handbook of Mathematical Functions" (off by at most 1.5e-7, half of that here), which shares its exponential with the density.
+__device__ __forceinline__ void normal2(float2 v, float2* density, float2* integral) {
+    const float2 a = make_float2(fabsf(v.x), fabsf(v.y));
+    const float2 e = exp2_2(mul2(mul2(v, v), both(-0.5f * kLog2e)));
+    const float2 t = rcp2(fma2(a, both(0.3275911f * 0.7071067811865476f), both(1.0f)));
+    float2 s = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    s = fma2(t, s, both(0.5f * 1.421413741f));
+    s = fma2(t, s, both(0.5f * -0.284496736f));
+    s = fma2(t, s, both(0.5f * 0.254829592f));
+    const float2 tail = mul2(mul2(t, e), s), rest = fma2(tail, both(-1.0f), both(1.0f));
+    *integral = make_float2(v.x < 0.0f ? tail.x : rest.x, v.y < 0.0f ? tail.y : rest.y);
+    *density = mul2(e, both(0.3989422804014327f));
 }
 
 // act(v).  GELU by tanh: v (1 + tanh(t)) / 2 = v sigmoid(2 t) with t = c (v + a v^3).  A NaN is 0 behind ReLU and ReLU6, as in the
 // other kernels.
 template <int ACT>
-__device__ __forceinline__ float act_f(float v) {
-    if (ACT == DLF_ACT_RELU) return fmaxf(v, 0.0f);
-    if (ACT == DLF_ACT_RELU6) return fminf(fmaxf(v, 0.0f), 6.0f);
-    if (ACT == DLF_ACT_GELU) return v * normal_f(v).y;
-    if (ACT == DLF_ACT_GELU_TANH) return v * sigmoid_f(2.0f * kGeluC * (v + kGeluA * v * v * v));
-    if (ACT == DLF_ACT_SILU) return v * sigmoid_f(v);
+__device__ __forceinline__ float2 act2(float2 v) {
+    if (ACT == DLF_ACT_RELU) return make_float2(fmaxf(v.x, 0.0f), fmaxf(v.y, 0.0f));
+    if (ACT == DLF_ACT_RELU6) return make_float2(fminf(fmaxf(v.x, 0.0f), 6.0f), fminf(fmaxf(v.y, 0.0f), 6.0f));
+    if (ACT == DLF_ACT_GELU) {
+        float2 density, integral;
+        normal2(v, &density, &integral);
+        return mul2(v, integral);
+    }
+    if (ACT == DLF_ACT_GELU_TANH) return mul2(v, sigmoid2(mul2(v, fma2(mul2(v, v), both(2.0f * kGeluC * kGeluA), both(2.0f * kGeluC)))));
+    if (ACT == DLF_ACT_SILU) return mul2(v, sigmoid2(v));
     return v;
 }
 // act(v) and its derivative (0 at the corners of ReLU and ReLU6).
 template <int ACT>
-__device__ __forceinline__ float2 act_grad_f(float v) {
-    if (ACT == DLF_ACT_RELU) return make_float2(fmaxf(v, 0.0f), v > 0.0f ? 1.0f : 0.0f);
-    if (ACT == DLF_ACT_RELU6) return make_float2(fminf(fmaxf(v, 0.0f), 6.0f), v > 0.0f && v < 6.0f ? 1.0f : 0.0f);
+__device__ __forceinline__ void act_grad2(float2 v, float2* value, float2* slope) {
+    *value = v;
+    *slope = both(1.0f);
+    if (ACT == DLF_ACT_RELU) {
+        *value = act2<ACT>(v);
+        *slope = make_float2(v.x > 0.0f ? 1.0f : 0.0f, v.y > 0.0f ? 1.0f : 0.0f);
+    }
+    if (ACT == DLF_ACT_RELU6) {
+        *value = act2<ACT>(v);
+        *slope = make_float2(v.x > 0.0f && v.x < 6.0f ? 1.0f : 0.0f, v.y > 0.0f && v.y < 6.0f ? 1.0f : 0.0f);
+    }
     if (ACT == DLF_ACT_GELU) {
-        const float2 n = normal_f(v);
-        return make_float2(v * n.y, fmaf(v, n.x, n.y));
+        float2 density, integral;
+        normal2(v, &density, &integral);
+        *value = mul2(v, integral);
+        *slope = fma2(v, density, integral);
     }
-    if (ACT == DLF_ACT_GELU_TANH) {
-        const float s = sigmoid_f(2.0f * kGeluC * (v + kGeluA * v * v * v));
-        return make_float2(v * s, s + v * s * (1.0f - s) * (2.0f * kGeluC * (1.0f + 3.0f * kGeluA * v * v)));
+    if (ACT == DLF_ACT_GELU_TANH || ACT == DLF_ACT_SILU) {
+        // v s(t), s the sigmoid: s + v s (1 - s) t'
+        const float2 q = mul2(v, v);
+        const float2 t = ACT == DLF_ACT_SILU ? v : mul2(v, fma2(q, both(2.0f * kGeluC * kGeluA), both(2.0f * kGeluC)));
+        const float2 s = sigmoid2(t), w = fma2(s, both(-1.0f), both(1.0f));
+        *value = mul2(v, s);
+        const float2 dt = ACT == DLF_ACT_SILU ? w : mul2(w, fma2(q, both(6.0f * kGeluC * kGeluA), both(2.0f * kGeluC)));
+        *slope = fma2(*value, dt, s);
     }
-    if (ACT == DLF_ACT_SILU) {
-        const float s = sigmoid_f(v);
-        return make_float2(v * s, s * (1.0f + v * (1.0f - s)));
-    }
-    return make_float2(v, 1.0f);
 }
+template <int ACT>
+__device__ __forceinline__ float act_f(float v) { return act2<ACT>(make_float2(v, v)).x; }
 
 // Calls f with the activation as a compile-time constant: one branch for a run of values.
 template <typename F>

@@ -225,7 +225,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
                     if (p.o[1].p) put(1, v);
                     with_act(p.act, [&](auto act) {
 #pragma unroll
-                        for (int i = 0; i < 64; i++) v[i] = act_f<act.value>(v[i]);
+                        for (int i = 0; i < 64; i += 2) {
+                            const float2 a = act2<act.value>(make_float2(v[i], v[i + 1]));
+                            v[i] = a.x; v[i + 1] = a.y;
+                        }
                     });
                     put(0, v);
                 } else {
@@ -235,7 +238,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
                     if (p.o[2].p) put(2, u);
                     with_act(p.act, [&](auto act) {
 #pragma unroll
-                        for (int i = 0; i < 64; i++) v[i] = act_f<act.value>(v[i]) * u[i];
+                        for (int i = 0; i < 64; i += 2) {
+                            const float2 a = mul2(act2<act.value>(make_float2(v[i], v[i + 1])), make_float2(u[i], u[i + 1]));
+                            v[i] = a.x; v[i + 1] = a.y;
+                        }
                     });
                     put(0, v);
                 }

@@ -96,22 +96,6 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* s
                  ::"l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(src)), "r"(c0), "r"(c1) : "memory");
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    T v[2] = {from_f32<T>(a), from_f32<T>(b)};
-    return *reinterpret_cast<const uint32_t*>(v);
-}
-template <>
-__device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-template <>
-__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // A warp's 32 rows of 64 values from column col0 on, as they lie in memory, a lane its row: the first `cols` of them and, behind
 // those and the matrix's last row, zeros.  Rows that start off the 16-byte boundaries, or end between two, come through `stg`
 // (4096 bytes of the warp's own), whole runs of columns at a time.
