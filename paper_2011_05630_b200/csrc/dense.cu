@@ -7,6 +7,7 @@
 
 #include "dense.h"
 #include "dense_math.cuh"
+#include "dense_mem.cuh"
 #include "ptx.cuh"
 
 namespace cg = cooperative_groups;
@@ -183,19 +184,27 @@ template <typename T, int V>
 GradFn pick_grad(bool gated, int act) { return gated ? pick_grad_act<T, V, true>(act) : pick_grad_act<T, V, false>(act); }
 
 // ---- rows onto 16-byte boundaries --------------------------------------------------------------------------------------------
-// For an operand whose rows start anywhere: the tensor-core kernels load tiles by TMA, which takes 16-byte boundaries only.  A copy costs
-// 4 bytes a value once, where a product reads the operand's tiles many times.
-__global__ void __launch_bounds__(256) dense_pack_kernel(const unsigned short* from, int64_t ld_from, uint4* to, int64_t ld_to8, int64_t rows, int64_t cols) {
+// For operands whose rows start anywhere: the tensor-core kernels load tiles by TMA, which takes 16-byte boundaries only.  A copy costs
+// 4 bytes a value once, where a product reads the operand's tiles many times.  All of a call's operands in one launch; two aligned pieces
+// of 16 bytes are read for each piece written.
+struct PackParams {
+    DensePack job[kMaxPacks];
+    int64_t first[kMaxPacks + 1];   // pieces of 16 bytes before a job's
+    int n;
+};
+__global__ void __launch_bounds__(256) dense_pack_kernel(const __grid_constant__ PackParams p) {
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t per_row = (cols + 7) / 8, total = rows * per_row;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = i / per_row, c = (i - row * per_row) * 8;
-        const unsigned short* p = from + row * ld_from + c;
-        uint32_t v[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = c + e < cols ? ld_map(p + e) : 0u;
-        to[row * ld_to8 + c / 8] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < p.first[p.n]; i += static_cast<int64_t>(gridDim.x) * 256) {
+        int q = 0;
+        while (i >= p.first[q + 1]) q++;
+        const DensePack& d = p.job[q];
+        const int64_t per_row = (d.cols + 7) / 8, at = i - p.first[q], row = at / per_row, c = (at - row * per_row) * 8;
+        const unsigned short* from = static_cast<const unsigned short*>(d.from.p) + row * d.from.ld + c;
+        const int n = static_cast<int>(min(static_cast<int64_t>(8), d.cols - c));
+        Eight<true, true> v;
+        v.fetch(from, n);
+        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(const_cast<void*>(d.to.p)) + row * d.to.ld + c) = v.get(from, n);
     }
 }
 
@@ -263,12 +272,14 @@ int zero_vec(float* p, int64_t n, cudaStream_t s) {
 // ---- which kernel --------------------------------------------------------------------------------------------------------------
 // Microseconds among other kernels, for each kernel and layout that can run a product: fitted to 4000 measured times of 468 products
 // (forward, gated and both gradients, 5 to 2048 tokens, widths from 256 to 11264; root mean square of the logarithm 0.12 and
-// 0.09).  What is chosen by it takes 1.8 % longer than each product's best in the geometric mean, the best of the pairs alone 33 %, the
+// 0.09).  What is chosen by it takes 2.1 % longer than each product's best in the geometric mean, the best of the pairs alone 33 %, the
 // best of the clusters alone (where they can run at all) 10 %.
 double gemm_bytes(const DenseGemm& g) {
     const double m = static_cast<double>(g.M), n = static_cast<double>(g.N), k = static_cast<double>(g.K);
     return 2.0 * (m * k * std::max(g.sources, g.groups) + n * k * (g.gated ? 2 : g.sources) + m * n * g.groups);
 }
+// The longer of two times that overlap, a little more where they are near one another.
+double longer(double a, double b) { return std::pow(std::pow(a, 4.0) + std::pow(b, 4.0), 0.25); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
@@ -291,10 +302,10 @@ double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
             const double busy = std::min(two ? 2.0 : 1.0, std::max(1.0, static_cast<double>(ctas) / sms));   // CTAs of an SM at a time
             const double stage = (g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024) + c.bn * 128;
             // a chunk: its matrix instructions and what lies between two runs, its bytes at an SM's rate, a round trip shared by the ring
-            double chunk = std::max(0.15 + 0.00055 * c.bn, stage * busy / 123e3);
-            if (stages < share) chunk = std::max(chunk, 1.18 / stages);
-            const double one = 2.87 + share * chunk + (c.split > 1 ? 0.9 + 2.6e-4 * c.rows * c.bn : 9.2e-5 * c.rows * c.bn);
-            const double us = std::max(one + (waves - 1.0) * (one - (two ? 0.65 : 0.0)), 2.87 + gemm_bytes(g) / 4.6e6);
+            double chunk = std::max(0.136 + 0.0005 * c.bn, stage * busy / 122e3);
+            if (stages < share) chunk = std::max(chunk, 1.17 / stages);
+            const double one = 2.61 + share * chunk + (c.split > 1 ? 1.1 + 2.6e-4 * c.rows * c.bn : 9.4e-5 * c.rows * c.bn);
+            const double us = longer(one + (waves - 1.0) * (one - (two ? 0.42 : 0.0)), 2.61 + gemm_bytes(g) / 4.94e6);
             if (least < 0 || us < least) {
                 least = us;
                 *best = c;
@@ -306,8 +317,8 @@ double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
 double pair_cost(const DenseGemm& g, int sms, int bn) {
     const int64_t tiles = ceil_div(g.M, 256) * ceil_div(g.N, g.gated ? bn / 2 : bn) * g.groups;
     const double waves = static_cast<double>(ceil_div(tiles, std::max(1, sms / 2))), chunks = static_cast<double>(ceil_div(g.K, 64) * g.sources);
-    const double chunk = bn == 256 ? 0.312 : 0.275, rows = bn == 256 ? 3.0 : 2.35;   // (24 KB of a stage come no faster than 32)
-    return std::max(0.87 + waves * (chunks * chunk + 0.3 * rows) + rows, 0.87 + gemm_bytes(g) / 5.13e6);
+    const double chunk = bn == 256 ? 0.309 : 0.274, rows = bn == 256 ? 2.45 : 1.85;   // (24 KB of a stage come no faster than 32)
+    return longer(1.57 + waves * (chunks * chunk + 0.3 * rows) + rows, 1.57 + gemm_bytes(g) / 5.88e6);
 }
 
 int launch_gemm(const DenseGemm& g, cudaStream_t s) {
@@ -323,19 +334,15 @@ int launch_gemm(const DenseGemm& g, cudaStream_t s) {
 // An operand as the products read it: itself, or a copy in the workspace (`run`: made now).
 struct Operands {
     Carver& carve;
-    struct Copy { int64_t rows, cols; Mat from, to; } copies[4];
+    DensePack jobs[kMaxPacks];
     int n = 0;
     Mat operator()(const Mat& m, int64_t rows, int64_t cols) {
         if (!m.p || dense_rows16(m)) return m;
         const Mat to = carve.matrix(rows, cols);
-        copies[n++] = Copy{rows, cols, m, to};
+        jobs[n++] = DensePack{rows, cols, m, to};
         return to;
     }
-    int run(cudaStream_t s) const {
-        int rc = DLF_OK;
-        for (int i = 0; i < n && rc == DLF_OK; i++) rc = launch_dense_pack(copies[i].rows, copies[i].cols, copies[i].from, copies[i].to, s);
-        return rc;
-    }
+    int run(cudaStream_t s) const { return n ? launch_dense_pack(jobs, n, s) : DLF_OK; }
 };
 
 // ---- the four operators; with `need` they only say how much workspace they want ------------------------------------------------
@@ -521,14 +528,18 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
 
 }  // namespace
 
-int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to, cudaStream_t s) {
+int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s) {
     int sms = 0;
     const int rc = query_sms(&sms);
     if (rc) return rc;
-    const int64_t items = rows * ((cols + 7) / 8);
-    const int grid = static_cast<int>(std::min<int64_t>((items + 255) / 256, 8ll * sms));
-    const cudaError_t e = launch_kernel(dense_pack_kernel, grid, 256, 0, s, static_cast<const unsigned short*>(from.p), from.ld,
-                                        static_cast<uint4*>(const_cast<void*>(to.p)), to.ld / 8, rows, cols);
+    PackParams p{};
+    p.n = n;
+    for (int i = 0; i < n; i++) {
+        p.job[i] = jobs[i];
+        p.first[i + 1] = p.first[i] + jobs[i].rows * ceil_div(jobs[i].cols, 8);
+    }
+    const int grid = static_cast<int>(std::min<int64_t>(ceil_div(p.first[n], 256), 8ll * sms));
+    const cudaError_t e = launch_kernel(dense_pack_kernel, grid, 256, 0, s, p);
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 

@@ -61,7 +61,13 @@ int dense_lat_status(cudaStream_t s, int* code);
 bool dense_gemv_takes(int64_t m);                             // dense_gemv.cu: forward products of a few tokens, any rows
 int launch_dense_gemv(const DenseGemm& g, cudaStream_t s);
 
-int launch_dense_pack(int64_t rows, int64_t cols, const Mat& from, const Mat& to, cudaStream_t s);
+// Copies matrices to rows on 16-byte boundaries (zeros behind a row's end, up to the boundary).
+constexpr int kMaxPacks = 3;   // (x and both weight matrices)
+struct DensePack {
+    int64_t rows, cols;
+    Mat from, to;
+};
+int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s);
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s);
 
 }  // namespace dlf

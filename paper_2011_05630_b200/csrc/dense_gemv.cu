@@ -12,7 +12,8 @@
 
 #include "dense.h"
 #include "dense_math.cuh"
-#include "dense_tc.cuh"
+#include "dense_mem.cuh"
+#include "ptx.cuh"
 
 namespace dlf {
 
@@ -25,58 +26,6 @@ struct GemvParams {
     const float* bias[2];
     long long N;
     int M, K, act, rows;   // rows: weight rows of a CTA
-};
-
-// 16 bytes if `live`, else zeros: one predicated load, no branch.  Weights are read once: they do not push the tokens out of the
-// first-level cache.
-template <bool STREAM>
-__device__ __forceinline__ uint4 ld16_if(const void* p, bool live) {
-    uint4 v;
-    if (STREAM)
-        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
-                     "@q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-                     : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"(static_cast<int>(live)) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
-                     "@q ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-                     : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"(static_cast<int>(live)) : "memory");
-    return v;
-}
-
-// 8 consecutive values of a row, n of which exist (none for n <= 0, zeros for the others): on their way from fetch() on, put together
-// by get().  ANY: the row starts and ends anywhere (else n is a multiple of 8); the values are in one or two aligned pieces of 16 bytes (a piece that holds one of them
-// lies in memory that exists).
-template <bool ANY, bool STREAM>
-struct Eight;
-template <bool STREAM>
-struct Eight<false, STREAM> {
-    uint4 a;
-    __device__ __forceinline__ void fetch(const unsigned short* p, int n) { a = ld16_if<STREAM>(p, n > 0); }
-    __device__ __forceinline__ uint4 get(const unsigned short*, int) const { return a; }
-};
-template <bool STREAM>
-struct Eight<true, STREAM> {
-    uint4 a, b;
-    __device__ __forceinline__ void fetch(const unsigned short* p, int n) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p), s = at & 15;
-        a = ld16_if<STREAM>(reinterpret_cast<const void*>(at - s), n > 0);
-        b = ld16_if<STREAM>(reinterpret_cast<const void*>(at - s + 16), n > 0 && static_cast<int>(s) + 2 * min(n, 8) > 16);
-    }
-    __device__ __forceinline__ uint4 get(const unsigned short* p, int n) const {
-        const uintptr_t s = reinterpret_cast<uintptr_t>(p) & 15;
-        uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, w[4];
-#pragma unroll
-        for (int i = 0; i < 6; i++) v[i] = s & 8 ? v[i + 2] : v[i];
-#pragma unroll
-        for (int i = 0; i < 5; i++) v[i] = s & 4 ? v[i + 1] : v[i];
-#pragma unroll
-        for (int i = 0; i < 4; i++) w[i] = s & 2 ? __funnelshift_r(v[i], v[i + 1], 16) : v[i];
-        if (n < 8) {
-#pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xffffu : 0u;
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
 };
 
 template <typename T>

@@ -219,7 +219,19 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                     res[it] = ld_map(reinterpret_cast<const uint4*>(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c));
             }
         };
+        // ... and rows off the 16-byte boundaries 32 columns of a row at a time, side by side in a warp, kRows of them
+        constexpr int kRows = 16;
+        const int groups = out_bn / 32;   // (of columns)
+        float any[kRows];
+        auto fetch_any = [&](int i0) {
+#pragma unroll
+            for (int it = 0; it < kRows; it++) {
+                const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
+                any[it] = add && r < my_rows && c < n_cols ? to_f32(ld_map(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c)) : 0.0f;
+            }
+        };
         if (p.vec) fetch_res(threadIdx.x);
+        else fetch_any(warp);
         bool ok = mbar_wait_warp<true>(&tfull_bar, 0u, abort_flag, status, 0xA20 | (blockIdx.x << 12));
         tc_fence_after_sync();
         const int dest = SPLIT > 1 ? min(m / p.rows_per, SPLIT - 1) : 0, row = m - dest * p.rows_per;
@@ -304,22 +316,14 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                 }
             }
         } else if (ok) {
-            // rows off the 16-byte boundaries: a warp has 32 columns of a row at a time, side by side, and kRows of them on their way
-            constexpr int kRows = 8;
-            const int groups = out_bn / 32;   // (of columns)
 #pragma unroll 1
             for (int i0 = warp; i0 < my_rows * groups; i0 += kRows * kEpiWarps) {
-                float a[kRows];
-#pragma unroll
-                for (int it = 0; it < kRows; it++) {
-                    const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
-                    a[it] = add && r < my_rows && c < n_cols ? to_f32(ld_map(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c)) : 0.0f;
-                }
+                if (i0 != warp) fetch_any(i0);
 #pragma unroll
                 for (int it = 0; it < kRows; it++) {
                     const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
                     if (r >= my_rows || c >= n_cols) continue;
-                    float v[1], u[1], b[1] = {a[it]};
+                    float v[1], u[1], b[1] = {any[it]};
                     auto sum = [&](int col, float (&s)[1]) {
                         const uint32_t at = static_cast<uint32_t>(r * p.BN * 4) + ((static_cast<uint32_t>(col >> 2) ^ (static_cast<uint32_t>(r) & 7u)) << 4) + (col & 3) * 4;
                         s[0] = 0.0f;
