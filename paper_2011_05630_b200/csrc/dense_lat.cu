@@ -48,7 +48,7 @@ struct LatParams {
     bool vec;                          // every row that is read or written here starts on a 16-byte boundary
 };
 
-// From the sums of W outputs of a row to what is stored: v (and u of a gated tile), the biases, what is added.
+// From the sums of W (an even number) outputs of a row to what is stored: v (and u of a gated tile), the biases, what is added.
 template <int EPI, int W, typename PUT>
 __device__ __forceinline__ void finish(int act_code, float (&v)[W], float (&u)[W], const float (&r)[W], PUT&& put) {
     if (EPI == EPI_LINEAR) {
@@ -60,12 +60,11 @@ __device__ __forceinline__ void finish(int act_code, float (&v)[W], float (&u)[W
     if (EPI != EPI_PLAIN)
         with_act(act_code, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i + 1 < W; i += 2) {
+            for (int i = 0; i < W; i += 2) {
                 float2 a = act2<act.value>(make_float2(v[i], v[i + 1]));
                 if (EPI == EPI_GATED) a = mul2(a, make_float2(u[i], u[i + 1]));
                 v[i] = a.x; v[i + 1] = a.y;
             }
-            if (W % 2) v[W - 1] = EPI == EPI_GATED ? act_f<act.value>(v[W - 1]) * u[W - 1] : act_f<act.value>(v[W - 1]);
         });
     put(0, v);
 }
@@ -206,32 +205,48 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
             const float* b = p.bias[EPI == EPI_GATED && static_cast<int>(threadIdx.x) >= out_bn ? 1 : 0];
             bias_s[threadIdx.x] = b && c < n_cols ? ld_map(b + n0 + c) : 0.0f;
         }
+        // A run is 8 outputs that are a piece of 16 bytes in memory: where rows start off the 16-byte boundaries, a row's first and
+        // last runs are not whole.  Run i of this CTA: row and first column (of n_cols), negative behind the last run.
+        const int runs = p.vec ? 1 << lg : (1 << lg) + 1, total = my_rows * runs;
+        const unsigned short* const out0 = static_cast<const unsigned short*>(p.o[EPI == EPI_PLAIN ? group : 0].p) + row_first * p.o[EPI == EPI_PLAIN ? group : 0].ld + n0;
+        const int64_t out_ld = p.o[EPI == EPI_PLAIN ? group : 0].ld;
+        auto run_at = [&](auto vec, int i, int* c) {
+            if (i >= total) return -1;
+            if (vec.value) {
+                const int r = i >> lg;
+                *c = (i - (r << lg)) * 8;
+                return *c < n_cols ? r : -1;
+            }
+            const int r = i / runs;
+            *c = (i - r * runs) * 8 - static_cast<int>((reinterpret_cast<uintptr_t>(out0 + r * out_ld) >> 1) & 7);
+            return *c < n_cols && *c + 8 > 0 ? r : -1;
+        };
+        // 8 values of a row from column c on, those that exist
+        auto fetch8 = [&](auto vec, const unsigned short* q, int c) {
+            if (vec.value ? c + 8 <= n_cols : c >= 0 && c + 8 <= n_cols && (reinterpret_cast<uintptr_t>(q) & 15) == 0) return ld_map(reinterpret_cast<const uint4*>(q));
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int d = c + 2 * e;
+                w[e] = (d >= 0 && d < n_cols ? ld_map(q + 2 * e) : 0u) | (d + 1 >= 0 && d + 1 < n_cols ? static_cast<uint32_t>(ld_map(q + 2 * e + 1)) : 0u) << 16;
+            }
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        };
         // what a thread's next runs have to add is fetched kItems runs at a time, the first ones behind the products
         constexpr int kItems = 4;
         const bool add = EPI == EPI_LINEAR && p.res.p != nullptr;
-        uint4 res[kItems];
-        auto fetch_res = [&](int i0) {
+        uint4 res[kItems] = {};
+        auto fetch_res = [&](auto vec, int i0) {
 #pragma unroll
             for (int it = 0; it < kItems; it++) {
-                const int i = i0 + it * 32 * kEpiWarps, r = i >> lg, c = (i - (r << lg)) * 8;
+                int c = 0;
+                const int r = run_at(vec, i0 + it * 32 * kEpiWarps, &c);
                 res[it] = make_uint4(0u, 0u, 0u, 0u);
-                if (add && r < my_rows && c + 8 <= n_cols)
-                    res[it] = ld_map(reinterpret_cast<const uint4*>(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c));
+                if (add && r >= 0) res[it] = fetch8(vec, static_cast<const unsigned short*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c, c);
             }
         };
-        // ... and rows off the 16-byte boundaries 32 columns of a row at a time, side by side in a warp, kRows of them
-        constexpr int kRows = 16;
-        const int groups = out_bn / 32;   // (of columns)
-        float any[kRows];
-        auto fetch_any = [&](int i0) {
-#pragma unroll
-            for (int it = 0; it < kRows; it++) {
-                const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
-                any[it] = add && r < my_rows && c < n_cols ? to_f32(ld_map(static_cast<const T*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c)) : 0.0f;
-            }
-        };
-        if (p.vec) fetch_res(threadIdx.x);
-        else fetch_any(warp);
+        if (add && p.vec) fetch_res(std::true_type{}, threadIdx.x);
+        else if (add) fetch_res(std::false_type{}, threadIdx.x);
         bool ok = mbar_wait_warp<true>(&tfull_bar, 0u, abort_flag, status, 0xA20 | (blockIdx.x << 12));
         tc_fence_after_sync();
         const int dest = SPLIT > 1 ? min(m / p.rows_per, SPLIT - 1) : 0, row = m - dest * p.rows_per;
@@ -269,77 +284,65 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         if (SPLIT > 1) ok = mbar_wait<true>(&red_bar, 0u, &red_abort_s, status, 0xA30 | (blockIdx.x << 12), 4 * kWaitLimitNs) && ok;
         asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");   // (the biases; with one CTA the sums)
         const uint8_t* red = sbase + p.red_off;
-        if (ok && p.vec) {
+        auto finish_runs = [&](auto vec) {
 #pragma unroll 1
-            for (int i0 = threadIdx.x; i0 < my_rows << lg; i0 += kItems * 32 * kEpiWarps) {
-                if (i0 != static_cast<int>(threadIdx.x)) fetch_res(i0);
+            for (int i0 = threadIdx.x; i0 < total; i0 += kItems * 32 * kEpiWarps) {
+                if (add && i0 != static_cast<int>(threadIdx.x)) fetch_res(vec, i0);
 #pragma unroll
                 for (int it = 0; it < kItems; it++) {
-                    const int i = i0 + it * 32 * kEpiWarps, r = i >> lg, c = (i - (r << lg)) * 8;
-                    if (r >= my_rows || c >= n_cols) continue;
-                    const bool whole = c + 8 <= n_cols;
+                    int c = 0;
+                    const int r = run_at(vec, i0 + it * 32 * kEpiWarps, &c);
+                    if (r < 0) continue;
                     float v[8], u[8], a[8];
                     auto sum = [&](int col, float (&s)[8]) {
-                        const uint32_t at = static_cast<uint32_t>(r * p.BN * 4) + ((static_cast<uint32_t>(col >> 2) ^ (static_cast<uint32_t>(r) & 7u)) << 4);
+                        const uint8_t* const at = red + r * p.BN * 4;
+                        const uint32_t swap = static_cast<uint32_t>(r) & 7u;
 #pragma unroll
                         for (int e = 0; e < 8; e++) s[e] = 0.0f;
+                        if (vec.value) {
+                            const uint32_t x16 = (static_cast<uint32_t>(col >> 2) ^ swap) << 4;
 #pragma unroll
-                        for (int sp = 0; sp < SPLIT; sp++) {
-                            const float4 x = *reinterpret_cast<const float4*>(red + sp * slab + at), y = *reinterpret_cast<const float4*>(red + sp * slab + (at ^ 16u));
-                            s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
-                            s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+                            for (int sp = 0; sp < SPLIT; sp++) {
+                                const float4 x = *reinterpret_cast<const float4*>(at + sp * slab + x16), y = *reinterpret_cast<const float4*>(at + sp * slab + (x16 ^ 16u));
+                                s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+                                s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; e++) {
+                                const int d = min(max(col + e, 0), p.BN - 1);   // (a column that does not exist: any value)
+                                const uint8_t* const q = at + (((static_cast<uint32_t>(d) >> 2) ^ swap) << 4) + (d & 3) * 4;
+#pragma unroll
+                                for (int sp = 0; sp < SPLIT; sp++) s[e] += *reinterpret_cast<const float*>(q + sp * slab);
+                            }
                         }
                         if (EPI != EPI_PLAIN) {
 #pragma unroll
-                            for (int e = 0; e < 8; e++) s[e] += bias_s[col + e];
+                            for (int e = 0; e < 8; e++) s[e] += bias_s[vec.value ? col + e : min(max(col + e, 0), p.BN - 1)];
                         }
                     };
                     sum(c, v);
                     if (EPI == EPI_GATED) sum(out_bn + c, u);
-                    const long long at = row_first + r;
-                    const T* add_p = static_cast<const T*>(p.res.p) + at * p.res.ld + n0 + c;
                     const T* in = reinterpret_cast<const T*>(&res[it]);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) a[e] = !add ? 0.0f : whole ? to_f32(in[e]) : c + e < n_cols ? to_f32(ld_map(add_p + e)) : 0.0f;
+                    for (int e = 0; e < 8; e++) a[e] = add ? to_f32(in[e]) : 0.0f;
                     finish<EPI>(p.act, v, u, a, [&](int which, const float(&f)[8]) {
                         const Mat& o = p.o[EPI == EPI_PLAIN ? group : which];
                         if (!o.p) return;
-                        T* t = static_cast<T*>(const_cast<void*>(o.p)) + at * o.ld + n0 + c;
-                        if (whole) {
+                        T* t = static_cast<T*>(const_cast<void*>(o.p)) + (row_first + r) * o.ld + n0 + c;
+                        if (vec.value ? c + 8 <= n_cols : c >= 0 && c + 8 <= n_cols && (reinterpret_cast<uintptr_t>(t) & 15) == 0) {
                             *reinterpret_cast<uint4*>(t) = make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; e++)
-                                if (c + e < n_cols) t[e] = from_f32<T>(f[e]);
+                                if (c + e >= 0 && c + e < n_cols) t[e] = from_f32<T>(f[e]);
                         }
                     });
                 }
             }
-        } else if (ok) {
-#pragma unroll 1
-            for (int i0 = warp; i0 < my_rows * groups; i0 += kRows * kEpiWarps) {
-                if (i0 != warp) fetch_any(i0);
-#pragma unroll
-                for (int it = 0; it < kRows; it++) {
-                    const int i = i0 + it * kEpiWarps, r = i >> (lg - 2), c = (i & (groups - 1)) * 32 + lane;
-                    if (r >= my_rows || c >= n_cols) continue;
-                    float v[1], u[1], b[1] = {any[it]};
-                    auto sum = [&](int col, float (&s)[1]) {
-                        const uint32_t at = static_cast<uint32_t>(r * p.BN * 4) + ((static_cast<uint32_t>(col >> 2) ^ (static_cast<uint32_t>(r) & 7u)) << 4) + (col & 3) * 4;
-                        s[0] = 0.0f;
-#pragma unroll
-                        for (int sp = 0; sp < SPLIT; sp++) s[0] += *reinterpret_cast<const float*>(red + sp * slab + at);
-                        if (EPI != EPI_PLAIN) s[0] += bias_s[col];
-                    };
-                    sum(c, v);
-                    if (EPI == EPI_GATED) sum(out_bn + c, u);
-                    finish<EPI>(p.act, v, u, b, [&](int which, const float(&f)[1]) {
-                        const Mat& o = p.o[EPI == EPI_PLAIN ? group : which];
-                        if (o.p) static_cast<T*>(const_cast<void*>(o.p))[(row_first + r) * o.ld + n0 + c] = from_f32<T>(f[0]);
-                    });
-                }
-            }
-        }
+        };
+        if (ok && p.vec) finish_runs(std::true_type{});
+        else if (ok) finish_runs(std::false_type{});
         tc_fence_before_sync();
     }
     __syncwarp();

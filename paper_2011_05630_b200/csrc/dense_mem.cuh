@@ -22,6 +22,18 @@ __device__ __forceinline__ uint4 ld16_if(const void* p, bool live) {
     return v;
 }
 
+// 16 of the 32 bytes of two pieces, from byte s on (an even number below 16).
+__device__ __forceinline__ uint4 shift16(const uint4& a, const uint4& b, uint32_t s) {
+    uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, w[4];
+#pragma unroll
+    for (int i = 0; i < 6; i++) v[i] = s & 8 ? v[i + 2] : v[i];
+#pragma unroll
+    for (int i = 0; i < 5; i++) v[i] = s & 4 ? v[i + 1] : v[i];
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = s & 2 ? __funnelshift_r(v[i], v[i + 1], 16) : v[i];
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // 8 consecutive values of a row, n of which exist (none for n <= 0, zeros for the others): on their way from fetch() on, put together
 // by get().  ANY: the row starts and ends anywhere (else n is a multiple of 8); the values are in one or two aligned pieces of 16 bytes (a piece that holds one of them
 // lies in memory that exists).
@@ -42,19 +54,14 @@ struct Eight<true, STREAM> {
         b = ld16_if<STREAM>(reinterpret_cast<const void*>(at - s + 16), n > 0 && static_cast<int>(s) + 2 * min(n, 8) > 16);
     }
     __device__ __forceinline__ uint4 get(const unsigned short* p, int n) const {
-        const uintptr_t s = reinterpret_cast<uintptr_t>(p) & 15;
-        uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, w[4];
-#pragma unroll
-        for (int i = 0; i < 6; i++) v[i] = s & 8 ? v[i + 2] : v[i];
-#pragma unroll
-        for (int i = 0; i < 5; i++) v[i] = s & 4 ? v[i + 1] : v[i];
-#pragma unroll
-        for (int i = 0; i < 4; i++) w[i] = s & 2 ? __funnelshift_r(v[i], v[i + 1], 16) : v[i];
+        uint4 q = shift16(a, b, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u);
         if (n < 8) {
+            uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int i = 0; i < 4; i++) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xffffu : 0u;
+            q = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        return q;
     }
 };
 

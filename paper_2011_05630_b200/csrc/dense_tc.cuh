@@ -8,6 +8,7 @@
 
 #include "dense.h"
 #include "dense_math.cuh"
+#include "dense_mem.cuh"
 #include "ptx.cuh"
 
 namespace dlf {
@@ -171,14 +172,25 @@ __device__ __forceinline__ void store_rows64(const Mat& o, const CUtensorMap* ma
         }
     } else {
         __syncwarp();
+        // a row's runs of 8 values begin where memory's pieces of 16 bytes do: nine runs a row, the first and the last not whole
         const int rows = static_cast<int>(min(static_cast<int64_t>(32), rows_end - row0));
-        T* p = static_cast<T*>(const_cast<void*>(o.p)) + row0 * o.ld + col0;
-        for (int r = 0; r < rows; r++, p += o.ld)
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int c = lane + h * 32;
-                if (c < cols) p[c] = *reinterpret_cast<const T*>(stg + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2);
+        unsigned short* const p0 = static_cast<unsigned short*>(const_cast<void*>(o.p)) + row0 * o.ld + col0;
+#pragma unroll 3
+        for (int it = 0; it < 9; it++) {
+            const int i = it * 32 + lane, r = i / 9;
+            unsigned short* const p = p0 + r * o.ld;
+            const int c = (i - r * 9) * 8 - static_cast<int>((reinterpret_cast<uintptr_t>(p) >> 1) & 7);   // its first column
+            if (r >= rows || c >= cols || c + 8 <= 0) continue;
+            const uint8_t* const row = stg + r * 128;
+            if (c >= 0 && c + 8 <= cols) {
+                const int k = c >> 3;
+                const uint4 a = *reinterpret_cast<const uint4*>(row + ((k ^ (r & 7)) << 4)), b = *reinterpret_cast<const uint4*>(row + (((k + 1) & 7) ^ (r & 7)) * 16);
+                *reinterpret_cast<uint4*>(p + c) = shift16(a, b, static_cast<uint32_t>(c & 7) * 2);
+            } else {
+                for (int e = max(0, -c); e < 8 && c + e < cols; e++)
+                    p[c + e] = *reinterpret_cast<const unsigned short*>(row + ((((c + e) >> 3) ^ (r & 7)) << 4) + ((c + e) & 7) * 2);
             }
+        }
         __syncwarp();
     }
 }
