@@ -305,7 +305,8 @@ int dlf_conv_chain_run_static(const dlf_layer_desc* layers, int n_layers, int N,
  *
  * Optional (null): bias, res, z, bg, bu, g, u of the forward calls; every output of the backward calls, and the inputs that
  * none of the outputs asked for needs (z without an activation, w without dx, x without dw, and so on).  y may be res itself
- * (same pointer and ld), dz may be dy or z; else no output may overlap an input or another output.
+ * (same pointer and ld), dz may be dy or z (likewise); else no output may overlap an input or another output (one that starts where
+ * another starts is refused).
  * m may be 0 (weights' and biases' gradients are then 0); n and k are at least 1; no size exceeds 2^30.
  * Pointers need the alignment of their element only.  Rows that start on 16-byte boundaries (pointer 16-byte aligned, ld a
  * multiple of 8) are fastest.

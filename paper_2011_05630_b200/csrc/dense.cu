@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 #include "dense.h"
@@ -238,6 +239,18 @@ struct Mats {
     }
 };
 
+// True if an output is an input or another output (the pairs that may be the same are left out by the caller).
+bool shared(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+    for (auto o = outputs.begin(); o != outputs.end(); o++) {
+        if (!*o) continue;
+        for (auto q = outputs.begin(); q != o; q++)
+            if (*q == *o) return true;
+        for (const void* i : inputs)
+            if (i == *o) return true;
+    }
+    return false;
+}
+
 // Hands out 256-byte aligned pieces of a workspace; with a null base it only counts.
 struct Carver {
     unsigned char* base;
@@ -271,8 +284,8 @@ int zero_vec(float* p, int64_t n, cudaStream_t s) {
 
 // ---- which kernel --------------------------------------------------------------------------------------------------------------
 // Microseconds among other kernels, for each kernel and layout that can run a product: fitted to 4000 measured times of 468 products
-// (forward, gated and both gradients, 5 to 2048 tokens, widths from 256 to 11264; root mean square of the logarithm 0.12 and
-// 0.09).  What is chosen by it takes 2.1 % longer than each product's best in the geometric mean, the best of the pairs alone 33 %, the
+// (forward, gated and both gradients, 5 to 2048 tokens, widths from 256 to 11264; root mean square of the logarithm 0.11 and
+// 0.09).  What is chosen by it takes 2.0 % longer than each product's best in the geometric mean, the best of the pairs alone 33 %, the
 // best of the clusters alone (where they can run at all) 10 %.
 double gemm_bytes(const DenseGemm& g) {
     const double m = static_cast<double>(g.M), n = static_cast<double>(g.N), k = static_cast<double>(g.K);
@@ -282,8 +295,13 @@ double gemm_bytes(const DenseGemm& g) {
 double longer(double a, double b) { return std::pow(std::pow(a, 4.0) + std::pow(b, 4.0), 0.25); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// 1 if rows start off the 128-byte lines: a tile's row of 128 bytes then takes two of them (777 x 1000 x 1001: 8.9 us with x's rows 1024
+// values apart, 10.0 with 1000).
+double off_lines(const Mat (&m)[2]) { return (m[0].ld | (m[1].p ? m[1].ld : 0)) % 64 != 0 ? 1.0 : 0.0; }
+
 double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
     double least = -1.0;
+    const double off_a = off_lines(g.a), off_b = off_lines(g.b);
     const int64_t tiles_m = ceil_div(g.M, 128), chunks = ceil_div(g.K, 64) * g.sources;
     DenseLatChoice c{};
     c.rows = g.a_mn ? static_cast<int>(std::min<int64_t>(g.M, 128)) : static_cast<int>(ceil_div(g.M, tiles_m));
@@ -300,12 +318,12 @@ double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
             const double slots = sms * (c.split == 1 ? (two ? 2.0 : 1.0) : c.split == 2 ? 1.0 : c.split == 4 ? 132.0 / 148 : 120.0 / 148);
             const double waves = std::ceil(static_cast<double>(ctas) / slots), share = static_cast<double>(ceil_div(chunks, c.split));
             const double busy = std::min(two ? 2.0 : 1.0, std::max(1.0, static_cast<double>(ctas) / sms));   // CTAs of an SM at a time
-            const double stage = (g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024) + c.bn * 128;
+            const double stage = (g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024) * (1.0 + 0.54 * off_a) + c.bn * 128 * (1.0 + 0.54 * off_b);
             // a chunk: its matrix instructions and what lies between two runs, its bytes at an SM's rate, a round trip shared by the ring
-            double chunk = std::max(0.136 + 0.0005 * c.bn, stage * busy / 122e3);
+            double chunk = std::max(0.141 + 0.0004 * c.bn, stage * busy / 126e3);
             if (stages < share) chunk = std::max(chunk, 1.17 / stages);
-            const double one = 2.61 + share * chunk + (c.split > 1 ? 1.1 + 2.6e-4 * c.rows * c.bn : 9.4e-5 * c.rows * c.bn);
-            const double us = longer(one + (waves - 1.0) * (one - (two ? 0.42 : 0.0)), 2.61 + gemm_bytes(g) / 4.94e6);
+            const double one = 2.61 + share * chunk + (c.split > 1 ? 1.1 + 2.5e-4 * c.rows * c.bn : 8.5e-5 * c.rows * c.bn);
+            const double us = longer(one + (waves - 1.0) * (one - (two ? 0.54 : 0.0)), 2.61 + gemm_bytes(g) / 4.84e6);
             if (least < 0 || us < least) {
                 least = us;
                 *best = c;
@@ -317,8 +335,8 @@ double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
 double pair_cost(const DenseGemm& g, int sms, int bn) {
     const int64_t tiles = ceil_div(g.M, 256) * ceil_div(g.N, g.gated ? bn / 2 : bn) * g.groups;
     const double waves = static_cast<double>(ceil_div(tiles, std::max(1, sms / 2))), chunks = static_cast<double>(ceil_div(g.K, 64) * g.sources);
-    const double chunk = bn == 256 ? 0.309 : 0.274, rows = bn == 256 ? 2.45 : 1.85;   // (24 KB of a stage come no faster than 32)
-    return longer(1.57 + waves * (chunks * chunk + 0.3 * rows) + rows, 1.57 + gemm_bytes(g) / 5.88e6);
+    const double chunk = (bn == 256 ? 0.308 : 0.272) * (1.0 + 0.05 * (off_lines(g.a) + off_lines(g.b))), rows = bn == 256 ? 2.43 : 1.83;   // (24 KB of a stage come no faster than 32)
+    return longer(1.56 + waves * (chunks * chunk + 0.3 * rows) + rows, 1.56 + gemm_bytes(g) / 5.79e6);
 }
 
 int launch_gemm(const DenseGemm& g, cudaStream_t s) {
@@ -362,6 +380,7 @@ int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, 
     g.out[0] = mat(a->y, a->m, a->n, a->ldy, a->m > 0);
     g.out[1] = mat(a->z, a->m, a->n, a->ldz, false);
     if (mat.rc) return mat.rc;
+    if (shared({a->y, a->z}, {a->x, a->w, a->bias}) || (a->res && (a->z == a->res || (a->y == a->res && a->m > 1 && a->ldy != a->ldres)))) return DLF_E_INVALID_ARG;
     if (need) *need = 0;
     if (a->m == 0) return DLF_OK;
     if (dense_gemv_takes(a->m)) return need ? DLF_OK : launch_dense_gemv(g, s);
@@ -387,6 +406,8 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
     const Mat dz_out = mat(a->dz, a->m, a->n, a->lddz, false);
     float* db = const_cast<float*>(mat.vec(a->db));
     if (mat.rc) return mat.rc;
+    if (shared({a->dx, a->dw, a->db, a->dz}, {a->x, a->w}) || shared({a->dx, a->dw, a->db}, {a->dy, has_act ? a->z : nullptr})) return DLF_E_INVALID_ARG;
+    if (some && a->m > 1 && a->dz && ((a->dz == a->dy && a->lddz != a->lddy) || (has_act && a->dz == a->z && a->lddz != a->ldz))) return DLF_E_INVALID_ARG;
     if (!some) {
         if (need) { *need = 0; return DLF_OK; }
         rc = zero_matrix(dw, a->n, a->k, s);
@@ -453,6 +474,7 @@ int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, si
     g.out[1] = mat(a->g, a->m, a->n, a->ldg, false);
     g.out[2] = mat(a->u, a->m, a->n, a->ldu, false);
     if (mat.rc) return mat.rc;
+    if (shared({a->h, a->g, a->u}, {a->x, a->wg, a->wu, a->bg, a->bu})) return DLF_E_INVALID_ARG;
     if (need) *need = 0;
     if (a->m == 0) return DLF_OK;
     if (dense_gemv_takes(a->m)) return need ? DLF_OK : launch_dense_gemv(g, s);
@@ -487,6 +509,7 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     d.db0 = const_cast<float*>(mat.vec(a->dbg));
     d.db1 = const_cast<float*>(mat.vec(a->dbu));
     if (mat.rc) return mat.rc;
+    if (shared({a->dx, a->dwg, a->dwu, a->dbg, a->dbu}, {a->dh, a->x, a->wg, a->wu, a->g, a->u})) return DLF_E_INVALID_ARG;
     if (!some) {
         if (need) { *need = 0; return DLF_OK; }
         rc = zero_matrix(dwg, a->n, a->k, s);

@@ -135,9 +135,9 @@ __device__ __forceinline__ void act_grad2(float2 v, float2* value, float2* slope
         *slope = fma2(v, density, integral);
     }
     if (ACT == DLF_ACT_GELU_TANH || ACT == DLF_ACT_SILU) {
-        // v s(t), s the sigmoid: s + v s (1 - s) t'
-        const float2 q = mul2(v, v);
-        const float2 t = ACT == DLF_ACT_SILU ? v : mul2(v, fma2(q, both(2.0f * kGeluC * kGeluA), both(2.0f * kGeluC)));
+        // v s(t), s the sigmoid: s + v s (1 - s) t'.  (Beyond 16 the sigmoid of GELU_TANH is 0 or 1, and v^2 need not be finite.)
+        const float2 c = ACT == DLF_ACT_SILU ? v : make_float2(fminf(fmaxf(v.x, -16.0f), 16.0f), fminf(fmaxf(v.y, -16.0f), 16.0f)), q = mul2(c, c);
+        const float2 t = ACT == DLF_ACT_SILU ? v : mul2(c, fma2(q, both(2.0f * kGeluC * kGeluA), both(2.0f * kGeluC)));
         const float2 s = sigmoid2(t), w = fma2(s, both(-1.0f), both(1.0f));
         *value = mul2(v, s);
         const float2 dt = ACT == DLF_ACT_SILU ? w : mul2(w, fma2(q, both(6.0f * kGeluC * kGeluA), both(2.0f * kGeluC)));

@@ -61,6 +61,17 @@ def test_refusals_of_one(make, kw, status):
     assert getattr(B.lib(), op)(args, 4096, 1 << 40, None) == status
 
 
+@pytest.mark.parametrize("make,kw", [
+    (linear, dict(y=P)), (linear, dict(z=2 * P)), (linear, dict(z=3 * P)), (linear, dict(res=3 * P, ldres=40)), (linear, dict(res=5 * P, z=5 * P)),
+    (linear_grad, dict(dx=2 * P)), (linear_grad, dict(dw=3 * P)), (linear_grad, dict(dx=P)), (linear_grad, dict(dw=4 * P)), (linear_grad, dict(dz=5 * P)),
+    (linear_grad, dict(dz=P, lddz=48)), (linear_grad, dict(dz=4 * P, lddz=48)), (linear_grad, dict(dz=2 * P)),
+    (gated, dict(h=P)), (gated, dict(g=4 * P)), (gated, dict(u=2 * P)), (gated, dict(g=8 * P, u=8 * P)),
+    (gated_grad, dict(dx=P)), (gated_grad, dict(dwg=9 * P)), (gated_grad, dict(dwu=4 * P)), (gated_grad, dict(dbg=7 * P)), (gated_grad, dict(dx=5 * P))])
+def test_outputs_over_inputs_are_refused(make, kw):
+    op, args = make(**kw)
+    assert getattr(B.lib(), op)(args, 4096, 1 << 40, None) == B.E_INVALID_ARG
+
+
 def test_null_arguments():
     for op in ("dlf_linear", "dlf_linear_grad", "dlf_gated", "dlf_gated_grad"):
         assert getattr(B.lib(), op)(None, None, 0, None) == B.E_INVALID_ARG

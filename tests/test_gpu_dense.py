@@ -1,5 +1,9 @@
 """Fully connected layers and gated blocks (dlf_linear, dlf_gated) and their backward passes against the formulas in 64 bits: both
 types, sizes from one to beyond a tile, odd ones, strides, empty batches; sums that are exact, infinities, streams, graphs."""
+import os
+import subprocess
+import sys
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -84,7 +88,7 @@ def check_gated_backward(mk, m, k, n, a, bias, pads=(0, 0, 0), shift=0):
         D.check(dbu, du.sum(0), su.sum(0) + D.sum_slack(m, du.abs().sum(0)), "dbu")
 
 
-SIZES = [(1, 1, 1), (1, 8, 8), (1, 2048, 1000), (2, 64, 64), (3, 65, 63), (4, 1024, 256), (5, 100, 37), (7, 200, 130), (8, 512, 264), (9, 72, 1000), (15, 129, 257),
+SIZES = [(1, 1, 1), (40, 1, 1), (300, 1, 64), (300, 64, 1), (1, 8, 8), (1, 2048, 1000), (2, 64, 64), (3, 65, 63), (4, 1024, 256), (5, 100, 37), (7, 200, 130), (8, 512, 264), (9, 72, 1000), (15, 129, 257),
          (16, 4096, 512), (17, 640, 384), (32, 1160, 520), (33, 64, 2048), (63, 256, 256), (64, 2050, 128), (65, 96, 72), (100, 712, 129), (127, 128, 127),
          (128, 1088, 256), (129, 127, 255), (200, 333, 1000), (255, 64, 513), (256, 768, 768), (257, 520, 1032), (300, 1000, 1001), (520, 264, 136), (777, 1000, 300), (1030, 192, 2056)]
 
@@ -216,6 +220,64 @@ def test_infinities_and_nan_stay_in_their_rows(m):
         keep = [i for i in range(m) if i != row]
         assert torch.equal(before[keep], after[keep])
     assert bool((dense.linear(x, w, act="relu")[row] == 0).all()) and bool((dense.linear(x, w, act="relu6")[row] == 0).all())   # (as in every kernel here)
+
+
+@pytest.mark.parametrize("a", ["relu6", "gelu", "gelu_tanh", "silu"])
+def test_large_and_small_values(a):
+    """Sums of any size a bf16 can hold: activations and their derivatives at both ends, and at nothing."""
+    v = torch.tensor([0.0, -0.0, 1e-38, 1e-6, 0.5, 3.0, 5.99, 6.0, 8.0, 16.0, 40.0, 90.0, 1e4, 1e20, 1e38], device="cuda")
+    v = torch.cat([v, -v]).to(torch.bfloat16)
+    for m in (1, 30, 300):
+        w = torch.zeros((v.numel(), 8), device="cuda", dtype=torch.bfloat16)
+        w[:, 0] = v
+        x = torch.zeros((m, 8), device="cuda", dtype=torch.bfloat16)
+        x[:, 0] = 1.0
+        y, z = dense.linear(x, w, act=a, save=True)
+        assert torch.equal(z, v.expand(m, -1))
+        want = D.act(v.double(), a).expand(m, -1)
+        D.check(y, want, D.ACT_ERR * (want.abs() + v.double().abs().clamp(max=16.0)), "y")   # (from 16 on it is v or 0 to the last bit)
+        dy = torch.ones_like(y)
+        dr = dense.linear_backward(dy, None, None, z, act=a, bias=False, residual=True, need_dx=False, need_dw=False)[3]
+        slope = D.act_grad(v.double().clamp(-1e6, 1e6), a).expand(m, -1)
+        D.check(dr, slope, D.ACT_ERR * (1 + v.double().abs().clamp(max=16.0)).expand(m, -1), "slope")
+
+
+def test_dz_over_dy_and_over_z():
+    """The C ABI lets dz take the place of dy or of z."""
+    from paper_2011_05630_b200 import binding as B
+    mk = Maker(3, torch.float16)
+    m, k, n = 200, 136, 264
+    dy, x, w, z = mk.mat(m, n), mk.mat(m, k), mk.mat(n, k), mk.mat(m, n)
+    want = dense.linear_backward(dy, x, w, z, act="gelu", residual=True)
+    for place in (dy.clone(), z.clone()):
+        d, zz = (place, z) if torch.equal(place, dy) else (dy, place)
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        args = dense._LINEAR_GRAD.pack(0, B.DENSE_ACTS["gelu"], m, k, n, d.data_ptr(), x.data_ptr(), w.data_ptr(), zz.data_ptr(), dx.data_ptr(), dw.data_ptr(),
+                                       0, place.data_ptr(), n, k, k, n, k, k, n)
+        B._check(B.lib().dlf_linear_grad(args, None, 0, torch.cuda.current_stream().cuda_stream), "dlf_linear_grad")
+        assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]) and torch.equal(place, want[3])
+    dense.synchronize()
+
+
+def test_captured_before_any_other_call():
+    """A process whose first calls are captured ones."""
+    code = """
+import torch
+from paper_2011_05630_b200 import dense
+x, w = torch.ones((40, 512), device="cuda").half(), torch.ones((264, 512), device="cuda").half()
+big = torch.ones((2048, 512), device="cuda").half()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    a, b, c = dense.linear(x, w), dense.gated(x[:3], w, w, act="relu"), dense.linear_backward(dense.linear(big, w), big, w)
+g.replay()
+dense.synchronize()
+assert bool((a == 512).all()) and bool((c[0] == 264 * 512).all() | torch.isinf(c[0]).all()) and bool(torch.isinf(b).all())
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
 
 
 @pytest.mark.parametrize("m", [4, 60, 400])
