@@ -119,13 +119,13 @@ def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, nee
     xp, ldx = _mat(x, "x", (m, k), dy)
     wp, ldw = _mat(w, "w", (n, k), dy)
     zp, ldz = _mat(z, "z", (m, n), dy) if a else (0, 0)
-    dx = dy.new_empty((m, k)) if need_dx else None
-    dw = dy.new_empty((n, k)) if need_dw else None
+    dx = (torch.empty_like(x) if x is not None else dy.new_empty((m, k))) if need_dx else None
+    dw = (torch.empty_like(w) if w is not None else dy.new_empty((n, k))) if need_dw else None
     db = dy.new_empty((n,), dtype=torch.float32) if bias else None
-    dr = dy.new_empty((m, n)) if residual and a else None
+    dr = torch.empty_like(dy) if residual and a else None
     ptr = lambda t: 0 if t is None else t.data_ptr()
     _call("dlf_linear_grad", _LINEAR_GRAD.pack(dtype, a, m, k, n, dyp, xp, wp, zp, ptr(dx), ptr(dw), ptr(db), ptr(dr),
-                                               lddy, ldx, ldw, ldz, k, k, n), dy, True)
+                                               lddy, ldx, ldw, ldz, k, k, n), dy, a != 0)
     return dx, dw, db, dy if residual and not a else dr
 
 
@@ -160,9 +160,8 @@ def gated_backward(dh, x, wg, wu, g, u, act="silu", bias=False, need_dx=True, ne
     wup, ldwu = _mat(wu, "wu", (n, k), dh)
     gp, ldg = _mat(g, "g", (m, n), dh)
     up, ldu = _mat(u, "u", (m, n), dh)
-    new = lambda rows: dh.new_empty((rows, k))
-    dx = new(m) if need_dx else None
-    dwg, dwu = (new(n), new(n)) if need_dw else (None, None)
+    dx = (torch.empty_like(x) if x is not None else dh.new_empty((m, k))) if need_dx else None
+    dwg, dwu = (torch.empty_like(wg) if wg is not None else dh.new_empty((n, k)) for _ in range(2)) if need_dw else (None, None)
     dbg, dbu = (dh.new_empty((n,), dtype=torch.float32) for _ in range(2)) if bias else (None, None)
     ptr = lambda t: 0 if t is None else t.data_ptr()
     _call("dlf_gated_grad", _GATED_GRAD.pack(dtype, a, m, k, n, dhp, xp, wgp, wup, gp, up, ptr(dx), ptr(dwg), ptr(dwu), ptr(dbg),
