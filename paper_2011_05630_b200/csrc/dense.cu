@@ -18,11 +18,11 @@ namespace dlf {
 namespace {
 
 // ---- gradients behind an activation ----------------------------------------------------------------------------------------
-// Bound by memory: 2 or 3 matrices are read, 1 or 2 written, once each.  A CTA owns 64 columns (128 bytes of a row: whole lines)
-// and walks rows, so that a column's sum stays in one thread's registers; kGradSplit CTAs share the rows of a strip as a cluster
+// Bound by memory: 2 or 3 matrices are read, 1 or 2 written, once each.  A CTA owns 64 columns (128 bytes of a row: whole lines; 16 where
+// a narrow matrix would leave SMs without work) and walks rows, so that a column's sum stays in one thread's registers; kGradSplit CTAs share the rows of a strip as a cluster
 // and their column sums meet in distributed shared memory, added up in the order of the ranks: the same bits every time, no
 // atomics and no second kernel.
-constexpr int kGradCols = 64, kGradThreads = 128, kGradSplit = 8;
+constexpr int kGradCols = 64, kNarrowCols = 16, kGradThreads = 128, kGradSplit = 8;
 
 // V values of a row, as they lie in memory: 8 on a 16-byte boundary, or 2 anywhere; `n` of them exist (of 8 all or none).
 template <typename T, int V>
@@ -58,25 +58,25 @@ struct Run<T, 2> {
     }
 };
 
-template <typename T, int V, bool GATED, int ACT>
+template <typename T, int V, bool GATED, int ACT, bool WIDE>
 __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThreads, GATED ? 5 : 7) dense_grad_kernel(const __grid_constant__ DenseGrad g) {
-    constexpr int TX = kGradCols / V, TY = kGradThreads / TX;
-    constexpr int kParts = V == 8 ? kGradThreads / 32 : TY;   // partial sums of a column: of a warp's four rows, or a thread's own
+    constexpr int kParts = kGradThreads / 32;   // partial sums of a column: a warp's
+    constexpr int width = WIDE ? kGradCols : kNarrowCols, tx_n = width / V;   // columns of the strip, threads of a row
     __shared__ float red[GATED ? 2 : 1][kParts][kGradCols];
     pdl_wait();
     pdl_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = static_cast<int>(cluster.block_rank());
     const int64_t strip = blockIdx.x / kGradSplit;
-    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
-    const int64_t col = strip * kGradCols + tx * V;
+    const int tx = threadIdx.x & (tx_n - 1), ty = threadIdx.x / tx_n;
+    const int64_t col = strip * width + tx * V;
     const int n = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(V), g.N - col)));   // (with V == 8 the columns are a multiple of 8)
     constexpr int VP = V / 2;   // pairs of values
     float2 s0[VP] = {}, s1[VP] = {};
     // rows are dealt out round by round, so that the CTAs of a strip are never far apart; the next kRows of a thread's rows are on their
     // way while these are worked on
     constexpr int kRows = V == 8 ? 2 : 4;
-    constexpr int64_t kStep = static_cast<int64_t>(TY) * kGradSplit;
+    constexpr int64_t rows_at_once = kGradThreads / tx_n, kStep = rows_at_once * kGradSplit;
     Run<T, V> dy[2][kRows], z[2][kRows], u[2][GATED ? kRows : 1];
     auto fetch = [&](int b, int64_t row0) {
 #pragma unroll
@@ -115,7 +115,7 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
         }
     };
     if (n > 0) {
-        int64_t row0 = static_cast<int64_t>(rank) * TY + ty;
+        int64_t row0 = rank * rows_at_once + ty;
         fetch(0, row0);
 #pragma unroll 1
         while (row0 < g.M) {
@@ -129,29 +129,28 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
         }
     }
     if (!g.db0 && !g.db1) return;   // (the same for every thread of the cluster)
-    if (V == 8) {   // (a warp has four rows of the strip's eight vectors)
-        auto meet = [](float2 v) {
+    // the rows of a warp
+    auto meet = [&](float2 v) {
 #pragma unroll
-            for (int d = 8; d < 32; d <<= 1) v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, d), __shfl_xor_sync(0xffffffffu, v.y, d)));
-            return v;
-        };
+        for (int d = tx_n; d < 32; d <<= 1) v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, d), __shfl_xor_sync(0xffffffffu, v.y, d)));
+        return v;
+    };
 #pragma unroll
-        for (int i = 0; i < VP; i++) {
-            s0[i] = meet(s0[i]);
-            if (GATED) s1[i] = meet(s1[i]);
-        }
+    for (int i = 0; i < VP; i++) {
+        s0[i] = meet(s0[i]);
+        if (GATED) s1[i] = meet(s1[i]);
     }
-    const int part = V == 8 ? static_cast<int>(threadIdx.x) / 32 : ty;
-    if (V != 8 || (threadIdx.x & 31) < TX) {
+    if (static_cast<int>(threadIdx.x & 31) < tx_n) {
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            red[0][part][tx * V + i] = i & 1 ? s0[i / 2].y : s0[i / 2].x;
-            if (GATED) red[GATED ? 1 : 0][part][tx * V + i] = i & 1 ? s1[i / 2].y : s1[i / 2].x;
+            red[0][threadIdx.x / 32][tx * V + i] = i & 1 ? s0[i / 2].y : s0[i / 2].x;
+            if (GATED) red[GATED ? 1 : 0][threadIdx.x / 32][tx * V + i] = i & 1 ? s1[i / 2].y : s1[i / 2].x;
         }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < (GATED ? 2 : 1) * kGradCols; i += kGradThreads) {
         const int which = i / kGradCols, c = i % kGradCols;
+        if (c >= width) continue;
         float s = 0.0f;
 #pragma unroll
         for (int y = 0; y < kParts; y++) s += red[which][y][c];
@@ -164,25 +163,28 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
             float s = 0.0f;
             for (int r = 0; r < kGradSplit; r++) s += *cluster.map_shared_rank(&red[which][0][c], r);
             float* db = which ? g.db1 : g.db0;
-            if (db && strip * kGradCols + c < g.N) db[strip * kGradCols + c] = s;
+            if (db && c < width && strip * width + c < g.N) db[strip * width + c] = s;
         }
     cluster.sync();   // no CTA leaves while its sums are still read
 }
 
 typedef void (*GradFn)(const DenseGrad);
-template <typename T, int V, bool GATED>
+template <typename T, int V, bool GATED, bool WIDE>
 GradFn pick_grad_act(int act) {
     switch (act) {
-        case DLF_ACT_RELU: return dense_grad_kernel<T, V, GATED, DLF_ACT_RELU>;
-        case DLF_ACT_RELU6: return dense_grad_kernel<T, V, GATED, DLF_ACT_RELU6>;
-        case DLF_ACT_GELU: return dense_grad_kernel<T, V, GATED, DLF_ACT_GELU>;
-        case DLF_ACT_GELU_TANH: return dense_grad_kernel<T, V, GATED, DLF_ACT_GELU_TANH>;
-        case DLF_ACT_SILU: return dense_grad_kernel<T, V, GATED, DLF_ACT_SILU>;
-        default: return dense_grad_kernel<T, V, GATED, DLF_ACT_NONE>;
+        case DLF_ACT_RELU: return dense_grad_kernel<T, V, GATED, DLF_ACT_RELU, WIDE>;
+        case DLF_ACT_RELU6: return dense_grad_kernel<T, V, GATED, DLF_ACT_RELU6, WIDE>;
+        case DLF_ACT_GELU: return dense_grad_kernel<T, V, GATED, DLF_ACT_GELU, WIDE>;
+        case DLF_ACT_GELU_TANH: return dense_grad_kernel<T, V, GATED, DLF_ACT_GELU_TANH, WIDE>;
+        case DLF_ACT_SILU: return dense_grad_kernel<T, V, GATED, DLF_ACT_SILU, WIDE>;
+        default: return dense_grad_kernel<T, V, GATED, DLF_ACT_NONE, WIDE>;
     }
 }
 template <typename T, int V>
-GradFn pick_grad(bool gated, int act) { return gated ? pick_grad_act<T, V, true>(act) : pick_grad_act<T, V, false>(act); }
+GradFn pick_grad(bool gated, bool wide, int act) {
+    if (gated) return wide ? pick_grad_act<T, V, true, true>(act) : pick_grad_act<T, V, true, false>(act);
+    return wide ? pick_grad_act<T, V, false, true>(act) : pick_grad_act<T, V, false, false>(act);
+}
 
 // ---- rows onto 16-byte boundaries --------------------------------------------------------------------------------------------
 // For operands whose rows start anywhere: the tensor-core kernels load tiles by TMA, which takes 16-byte boundaries only.  A copy costs
@@ -569,11 +571,16 @@ int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s) {
 int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
     auto vec = [](const Mat& m) { return !m.p || (aligned(16, m.p) && m.ld % 8 == 0); };
     const bool v8 = g.N % 8 == 0 && vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
-    const int64_t blocks = (g.N + kGradCols - 1) / kGradCols * kGradSplit;   // (at most 2^27)
-    const int grid = static_cast<int>(blocks);
+    int sms = 0;
+    const int rc = query_sms(&sms);
+    if (rc) return rc;
+    // Strips of 64 columns where they give every SM two CTAs or the rows are few, else of 16 (6428 rows of 128 columns 13.4 -> 6.1 us, 20000
+    // of 33 116 -> 44; but 512 of 1024 3.4 -> 4.6).
+    const bool wide = ceil_div(g.N, kGradCols) * kGradSplit >= 2 * sms || g.M < 1000;
+    const int grid = static_cast<int>(ceil_div(g.N, wide ? kGradCols : kNarrowCols) * kGradSplit);   // (at most 2^29)
     GradFn fn = nullptr;
-    if (g.dtype == DLF_BF16) fn = v8 ? pick_grad<__nv_bfloat16, 8>(g.gated, g.act) : pick_grad<__nv_bfloat16, 2>(g.gated, g.act);
-    else fn = v8 ? pick_grad<__half, 8>(g.gated, g.act) : pick_grad<__half, 2>(g.gated, g.act);
+    if (g.dtype == DLF_BF16) fn = v8 ? pick_grad<__nv_bfloat16, 8>(g.gated, wide, g.act) : pick_grad<__nv_bfloat16, 2>(g.gated, wide, g.act);
+    else fn = v8 ? pick_grad<__half, 8>(g.gated, wide, g.act) : pick_grad<__half, 2>(g.gated, wide, g.act);
     const cudaError_t e = launch_kernel(fn, grid, kGradThreads, 0, s, g);
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
