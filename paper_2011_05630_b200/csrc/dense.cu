@@ -205,9 +205,7 @@ __global__ void __launch_bounds__(256) dense_pack_kernel(const __grid_constant__
         const int64_t per_row = (d.cols + 7) / 8, at = i - p.first[q], row = at / per_row, c = (at - row * per_row) * 8;
         const unsigned short* from = static_cast<const unsigned short*>(d.from.p) + row * d.from.ld + c;
         const int n = static_cast<int>(min(static_cast<int64_t>(8), d.cols - c));
-        Eight<true, true> v;
-        v.fetch(from, n);
-        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(const_cast<void*>(d.to.p)) + row * d.to.ld + c) = v.get(from, n);
+        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(const_cast<void*>(d.to.p)) + row * d.to.ld + c) = load8_any(from, n);
     }
 }
 
@@ -385,7 +383,7 @@ int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, 
     if (shared({a->y, a->z}, {a->x, a->w, a->bias}) || (a->res && (a->z == a->res || (a->y == a->res && a->m > 1 && a->ldy != a->ldres)))) return DLF_E_INVALID_ARG;
     if (need) *need = 0;
     if (a->m == 0) return DLF_OK;
-    if (dense_gemv_takes(a->m)) return need ? DLF_OK : launch_dense_gemv(g, s);
+    if (dense_gemv_takes(g)) return need ? DLF_OK : launch_dense_gemv(g, s);
     Carver carve{static_cast<unsigned char*>(ws)};
     Operands op{carve};
     g.a[0] = op(g.a[0], a->m, a->k);
@@ -479,7 +477,7 @@ int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, si
     if (shared({a->h, a->g, a->u}, {a->x, a->wg, a->wu, a->bg, a->bu})) return DLF_E_INVALID_ARG;
     if (need) *need = 0;
     if (a->m == 0) return DLF_OK;
-    if (dense_gemv_takes(a->m)) return need ? DLF_OK : launch_dense_gemv(g, s);
+    if (dense_gemv_takes(g)) return need ? DLF_OK : launch_dense_gemv(g, s);
     Carver carve{static_cast<unsigned char*>(ws)};
     Operands op{carve};
     g.a[0] = op(g.a[0], a->m, a->k);

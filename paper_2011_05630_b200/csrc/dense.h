@@ -58,7 +58,7 @@ bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* stages
 int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s);
 int dense_lat_status(cudaStream_t s, int* code);
 
-bool dense_gemv_takes(int64_t m);                             // dense_gemv.cu: forward products of a few tokens, any rows
+bool dense_gemv_takes(const DenseGemm& g);                           // dense_gemv.cu: forward products of a few tokens, any rows
 int launch_dense_gemv(const DenseGemm& g, cudaStream_t s);
 
 // Copies matrices to rows on 16-byte boundaries (zeros behind a row's end, up to the boundary).

@@ -34,35 +34,17 @@ __device__ __forceinline__ uint4 shift16(const uint4& a, const uint4& b, uint32_
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// 8 consecutive values of a row, n of which exist (none for n <= 0, zeros for the others): on their way from fetch() on, put together
-// by get().  ANY: the row starts and ends anywhere (else n is a multiple of 8); the values are in one or two aligned pieces of 16 bytes (a piece that holds one of them
-// lies in memory that exists).
-template <bool ANY, bool STREAM>
-struct Eight;
-template <bool STREAM>
-struct Eight<false, STREAM> {
-    uint4 a;
-    __device__ __forceinline__ void fetch(const unsigned short* p, int n) { a = ld16_if<STREAM>(p, n > 0); }
-    __device__ __forceinline__ uint4 get(const unsigned short*, int) const { return a; }
-};
-template <bool STREAM>
-struct Eight<true, STREAM> {
-    uint4 a, b;
-    __device__ __forceinline__ void fetch(const unsigned short* p, int n) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p), s = at & 15;
-        a = ld16_if<STREAM>(reinterpret_cast<const void*>(at - s), n > 0);
-        b = ld16_if<STREAM>(reinterpret_cast<const void*>(at - s + 16), n > 0 && static_cast<int>(s) + 2 * min(n, 8) > 16);
-    }
-    __device__ __forceinline__ uint4 get(const unsigned short* p, int n) const {
-        uint4 q = shift16(a, b, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u);
-        if (n < 8) {
-            uint32_t w[4] = {q.x, q.y, q.z, q.w};
+// 8 consecutive values of a row from p on, n of which exist, zeros for the others: in one or two aligned pieces of 16 bytes (a piece that
+// holds one of them lies in memory that exists).
+__device__ __forceinline__ uint4 load8_any(const unsigned short* p, int n) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), s = at & 15;
+    const uint4 a = ld16_if<true>(reinterpret_cast<const void*>(at - s), n > 0);
+    const uint4 b = ld16_if<true>(reinterpret_cast<const void*>(at - s + 16), n > 0 && static_cast<int>(s) + 2 * min(n, 8) > 16);
+    const uint4 q = shift16(a, b, static_cast<uint32_t>(s));
+    uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xffffu : 0u;
-            q = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        return q;
-    }
-};
+    for (int i = 0; i < 4; i++) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xffffu : 0u;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
 }  // namespace dlf
