@@ -195,17 +195,28 @@ struct PackParams {
     int64_t first[kMaxPacks + 1];   // pieces of 16 bytes before a job's
     int n;
 };
+template <typename I>   // (what counts the pieces: a division in 64 bits costs several times the copy)
 __global__ void __launch_bounds__(256) dense_pack_kernel(const __grid_constant__ PackParams p) {
+    constexpr int kItems = 4;       // pieces of a thread on their way at a time
     pdl_wait();
     pdl_launch_dependents();
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < p.first[p.n]; i += static_cast<int64_t>(gridDim.x) * 256) {
-        int q = 0;
-        while (i >= p.first[q + 1]) q++;
+    for (int q = 0; q < p.n; q++) {
         const DensePack& d = p.job[q];
-        const int64_t per_row = (d.cols + 7) / 8, at = i - p.first[q], row = at / per_row, c = (at - row * per_row) * 8;
-        const unsigned short* from = static_cast<const unsigned short*>(d.from.p) + row * d.from.ld + c;
-        const int n = static_cast<int>(min(static_cast<int64_t>(8), d.cols - c));
-        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(const_cast<void*>(d.to.p)) + row * d.to.ld + c) = load8_any(from, n);
+        const I total = static_cast<I>(p.first[q + 1] - p.first[q]), per_row = static_cast<I>((d.cols + 7) / 8), threads = static_cast<I>(gridDim.x) * 256;
+        for (I i0 = static_cast<I>(blockIdx.x) * 256 + threadIdx.x; i0 < total; i0 += kItems * threads) {
+            uint4 v[kItems], *to[kItems];
+#pragma unroll
+            for (int e = 0; e < kItems; e++) {
+                const I i = i0 + e * threads, row = i / per_row, c = (i - row * per_row) * 8;
+                const bool in = i < total;
+                to[e] = reinterpret_cast<uint4*>(static_cast<unsigned short*>(const_cast<void*>(d.to.p)) + static_cast<int64_t>(row) * d.to.ld + c);
+                v[e] = load8_any(static_cast<const unsigned short*>(d.from.p) + static_cast<int64_t>(row) * d.from.ld + c,
+                                 in ? static_cast<int>(min(static_cast<int64_t>(8), d.cols - static_cast<int64_t>(c))) : 0);
+            }
+#pragma unroll
+            for (int e = 0; e < kItems; e++)
+                if (i0 + e * threads < total) *to[e] = v[e];
+        }
     }
 }
 
@@ -260,8 +271,9 @@ struct Carver {
         used += (bytes + 255) / 256 * 256;
         return p;
     }
+    // (rows on 128-byte lines: a tile's row of 128 bytes then is one of them)
     Mat matrix(int64_t rows, int64_t cols) {
-        const int64_t ld = (cols + 7) / 8 * 8;
+        const int64_t ld = (cols + 63) / 64 * 64;
         return Mat{(*this)(static_cast<size_t>(rows) * ld * 2), ld};
     }
 };
@@ -562,7 +574,7 @@ int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s) {
         p.first[i + 1] = p.first[i] + jobs[i].rows * ceil_div(jobs[i].cols, 8);
     }
     const int grid = static_cast<int>(std::min<int64_t>(ceil_div(p.first[n], 256), 8ll * sms));
-    const cudaError_t e = launch_kernel(dense_pack_kernel, grid, 256, 0, s, p);
+    const cudaError_t e = launch_kernel(p.first[n] < (1ll << 31) - (1ll << 24) ? dense_pack_kernel<uint32_t> : dense_pack_kernel<uint64_t>, grid, 256, 0, s, p);
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 

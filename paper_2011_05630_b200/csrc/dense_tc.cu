@@ -58,6 +58,121 @@ __device__ __forceinline__ TileAt tile_at(const PairParams& p, long long t) {
     return r;
 }
 
+// ---- a warp's rows between registers and memory ----
+// Rows that start anywhere into a warp's staging buffer, a row's columns side by side; zeros behind `rows` and `cols`.
+__device__ __noinline__ void rows64_in(const unsigned short* p, int64_t ld, uint8_t* stg, int lane, int rows, int cols) {
+#pragma unroll 8
+    for (int r = 0; r < 32; r++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int c = lane + h * 32;
+            const unsigned short v = r < rows && c < cols ? ld_map(p + r * ld + c) : static_cast<unsigned short>(0);
+            *reinterpret_cast<unsigned short*>(stg + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2) = v;
+        }
+}
+
+// A warp's 32 rows of 64 values from column col0 on, as they lie in memory, a lane its row: the first `cols` of them and, behind
+// those and the matrix's last row, zeros.  Rows that start off the 16-byte boundaries, or end between two, come through `stg`
+// (4096 bytes of the warp's own), whole runs of columns at a time.
+template <typename T>
+__device__ __forceinline__ void load_rows64(const Mat& m, bool vec, uint8_t* stg, int lane, int64_t row0, int64_t col0, int64_t rows_end, int cols, uint4 (&q)[8]) {
+    const unsigned short* p = static_cast<const unsigned short*>(m.p) + row0 * m.ld + col0;
+    const int rows = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(32), rows_end - row0)));
+    if (vec && (cols & 7) == 0) {
+        p += lane * m.ld;
+#pragma unroll
+        for (int j = 0; j < 8; j++) q[j] = lane < rows && j * 8 < cols ? ld_map(reinterpret_cast<const uint4*>(p + j * 8)) : make_uint4(0u, 0u, 0u, 0u);
+        return;
+    }
+    if (lane == 0) tma_store_wait_read();   // what lay here before has left
+    __syncwarp();
+    rows64_in(p, m.ld, stg, lane, rows, cols);
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; j++) q[j] = *reinterpret_cast<const uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4));
+    __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void add_row64(const uint4 (&q)[8], float* v) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const T* e = reinterpret_cast<const T*>(&q[j]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[j * 8 + i] += to_f32(e[i]);
+    }
+}
+__device__ __forceinline__ void add_bias64(const float* bias, int64_t col0, int cols, float* v) {
+    const float* b = bias + col0;
+    if (cols == 64 && (reinterpret_cast<uintptr_t>(b) & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const float4 f = ld_map(reinterpret_cast<const float4*>(b) + i);
+            v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 64; i++)
+            if (i < cols) v[i] += ld_map(b + i);
+    }
+}
+
+// A warp's staged rows (`rows` of 32, the first `cols` of 64 values) to rows that start anywhere, in memory's pieces of 16 bytes: of a row's 64
+// values the first ones up to a piece's start and the last ones, eight together, leave one by one, seven pieces between them
+// whole.  (Out of line: its registers are not the other path's.)
+__device__ __noinline__ void rows64_out(unsigned short* p0, int64_t ld, const uint8_t* stg, int lane, int rows, int cols) {
+    const auto head = [](const unsigned short* p) { return static_cast<int>((0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) >> 1)) & 7u); };
+    const auto at = [&](int r, int c) { return *reinterpret_cast<const unsigned short*>(stg + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2); };
+#pragma unroll
+    for (int it = 0; it < 7; it++) {
+        const int i = it * 32 + lane, r = i / 7;
+        unsigned short* const p = p0 + r * ld;
+        const int c = head(p) + (i - r * 7) * 8, k = c >> 3;
+        if (r >= rows || c >= cols) continue;
+        if (c + 8 <= cols) {
+            const uint8_t* const row = stg + r * 128;
+            const uint4 a = *reinterpret_cast<const uint4*>(row + ((k ^ (r & 7)) << 4)), b = *reinterpret_cast<const uint4*>(row + (((k + 1) & 7) ^ (r & 7)) * 16);
+            *reinterpret_cast<uint4*>(p + c) = shift16(a, b, static_cast<uint32_t>(c & 7) * 2);
+        } else {
+            for (int e = c; e < cols; e++) p[e] = at(r, e);
+        }
+    }
+#pragma unroll
+    for (int it = 0; it < 8; it++) {
+        const int i = it * 32 + lane, r = i >> 3, e = i & 7;
+        unsigned short* const p = p0 + r * ld;
+        const int c = e < head(p) ? e : 56 + e;
+        if (r < rows && c < cols) p[c] = at(r, c);
+    }
+}
+
+// A warp's 32 rows of 64 values (a lane holds a row): rounded, through `stg` (4096 bytes of the warp's own) and out, by a TMA store
+// where the output has a map, else row by row.  Rows and columns beyond the matrix are not written.  (A TMA store clips at the map's
+// edge in pieces of 16 bytes: with a last piece that is not whole it writes zeros behind the row's end.)
+template <typename T>
+__device__ __forceinline__ void store_rows64(const Mat& o, const CUtensorMap* map, bool tma, uint8_t* stg, int lane, int64_t row0, int64_t col0,
+                                             int64_t rows_end, int cols, const float* v) {
+    if (lane == 0) tma_store_wait_read();   // what lay here before has left
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const uint4 q = make_uint4(pack2<T>(v[8 * j], v[8 * j + 1]), pack2<T>(v[8 * j + 2], v[8 * j + 3]), pack2<T>(v[8 * j + 4], v[8 * j + 5]),
+                                   pack2<T>(v[8 * j + 6], v[8 * j + 7]));
+        *reinterpret_cast<uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) = q;
+    }
+    if (tma && (cols & 7) == 0) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(map, stg, static_cast<int>(col0), static_cast<int>(row0));
+            tma_store_commit();
+        }
+    } else {
+        __syncwarp();
+        rows64_out(static_cast<unsigned short*>(const_cast<void*>(o.p)) + row0 * o.ld + col0, o.ld, stg, lane, static_cast<int>(min(static_cast<int64_t>(32), rows_end - row0)), cols);
+        __syncwarp();
+    }
+}
+
 template <typename T, bool AMN, bool BMN, int EPI, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_pair_kernel(const __grid_constant__ PairParams p) {
     constexpr int kABytes = 128 * 128, kBRows = BN / 2, kBBytes = kBRows * 128, kStageBytes = kABytes + kBBytes, kStages = kRing / kStageBytes;

@@ -87,13 +87,13 @@ def need(op_args):
 
 def test_workspace():
     assert need(linear()) == 0 and need(gated()) == 0             # nothing where rows start on 16-byte boundaries
-    assert need(linear_grad()) == 256                             # dz: 4 x 32 values
+    assert need(linear_grad()) == 512                             # dz: 4 rows of 32 values, 64 apart
     assert need(linear_grad(act=0, z=0)) == 0 and need(linear_grad(dz=8 * P)) == 0
     assert need(linear_grad(dx=0, dw=0)) == 0 and need(linear_grad(m=0)) == 0
-    assert need(gated_grad()) == 512 and need(gated_grad(dx=0, dwu=0)) == 256
+    assert need(gated_grad()) == 1024 and need(gated_grad(dx=0, dwu=0)) == 512
     for op, args in (linear_grad(), gated_grad()):
         f = getattr(B.lib(), op)
-        assert f(args, None, 1 << 20, None) == B.E_WORKSPACE and f(args, 4096, 255, None) == B.E_WORKSPACE and f(args, 4096 + 16, 1 << 20, None) == B.E_WORKSPACE
+        assert f(args, None, 1 << 20, None) == B.E_WORKSPACE and f(args, 4096, 511, None) == B.E_WORKSPACE and f(args, 4096 + 16, 1 << 20, None) == B.E_WORKSPACE
 
 
 def test_tensors_off_the_device_are_refused():
