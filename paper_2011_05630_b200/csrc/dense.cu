@@ -311,54 +311,101 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // values apart, 10.0 with 1000).
 double off_lines(const Mat (&m)[2]) { return (m[0].ld | (m[1].p ? m[1].ld : 0)) % 64 != 0 ? 1.0 : 0.0; }
 
-double lat_cost(const DenseGemm& g, int sms, DenseLatChoice* best) {
+double lat_cost(const DenseGemm* g, int n, int sms, DenseLatChoice* best) {
     double least = -1.0;
-    const double off_a = off_lines(g.a), off_b = off_lines(g.b);
-    const int64_t tiles_m = ceil_div(g.M, 128), chunks = ceil_div(g.K, 64) * g.sources;
     DenseLatChoice c{};
-    c.rows = g.a_mn ? static_cast<int>(std::min<int64_t>(g.M, 128)) : static_cast<int>(ceil_div(g.M, tiles_m));
-    for (c.bn = 64; c.bn <= 128; c.bn += 64) {
-        const int64_t tiles = tiles_m * ceil_div(g.N, g.gated ? c.bn / 2 : c.bn) * g.groups;
+    for (c.bn = 64; c.bn <= 128; c.bn += 64)
         for (c.split = 1; c.split <= 8; c.split *= 2) {
-            const int64_t ctas = tiles * c.split;
-            if (ctas > (1 << 20)) break;
-            c.deep = ctas <= sms;
-            int stages = 0;
-            bool two = false;
-            if (!dense_lat_possible(g, c, &stages, &two)) continue;
+            int64_t ctas[2] = {}, all = 0;
+            for (int j = 0; j < n; j++) all += ctas[j] = ceil_div(g[j].M, 128) * ceil_div(g[j].N, g[j].gated ? c.bn / 2 : c.bn) * g[j].groups * c.split;
+            if (all > (1 << 20)) break;
+            c.deep = all <= sms;
+            int rows[2], stages[2];
+            bool two = true, possible = true;
+            for (int j = 0; j < n && possible; j++) {
+                bool fits = false;
+                possible = dense_lat_possible(g[j], c, &rows[j], &stages[j], &fits);
+                two = two && fits;
+            }
+            if (!possible) continue;
             // clusters find fewer places than single CTAs: 148, 132 and 120 CTAs of clusters of 2, 4 and 8 on 148 SMs
             const double slots = sms * (c.split == 1 ? (two ? 2.0 : 1.0) : c.split == 2 ? 1.0 : c.split == 4 ? 132.0 / 148 : 120.0 / 148);
-            const double waves = std::ceil(static_cast<double>(ctas) / slots), share = static_cast<double>(ceil_div(chunks, c.split));
-            const double busy = std::min(two ? 2.0 : 1.0, std::max(1.0, static_cast<double>(ctas) / sms));   // CTAs of an SM at a time
-            const double stage = (g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024) * (1.0 + 0.54 * off_a) + c.bn * 128 * (1.0 + 0.54 * off_b);
-            // a chunk: its matrix instructions and what lies between two runs, its bytes at an SM's rate, a round trip shared by the ring
-            double chunk = std::max(0.141 + 0.0004 * c.bn, stage * busy / 126e3);
-            if (stages < share) chunk = std::max(chunk, 1.17 / stages);
-            const double one = 2.61 + share * chunk + (c.split > 1 ? 1.1 + 2.5e-4 * c.rows * c.bn : 8.5e-5 * c.rows * c.bn);
-            const double us = longer(one + (waves - 1.0) * (one - (two ? 0.54 : 0.0)), 2.61 + gemm_bytes(g) / 4.84e6);
+            const double waves = std::ceil(static_cast<double>(all) / slots);
+            const double busy = std::min(two ? 2.0 : 1.0, std::max(1.0, static_cast<double>(all) / sms));   // CTAs of an SM at a time
+            double longest = 0.0, mean = 0.0, bytes = 0.0;
+            for (int j = 0; j < n; j++) {
+                const double share = static_cast<double>(ceil_div(ceil_div(g[j].K, 64) * g[j].sources, c.split));
+                const double stage = (g[j].a_mn ? 16384 : (rows[j] + 7) / 8 * 1024) * (1.0 + 0.54 * off_lines(g[j].a)) + c.bn * 128 * (1.0 + 0.54 * off_lines(g[j].b));
+                // a chunk: its matrix instructions and what lies between two runs, its bytes at an SM's rate, a round trip shared by the ring
+                double chunk = std::max(0.141 + 0.0004 * c.bn, stage * busy / 126e3);
+                if (stages[j] < share) chunk = std::max(chunk, 1.17 / stages[j]);
+                const double one = 2.61 + share * chunk + (c.split > 1 ? 1.1 + 2.5e-4 * rows[j] * c.bn : 8.5e-5 * rows[j] * c.bn);
+                longest = std::max(longest, one);
+                mean += one * static_cast<double>(ctas[j]) / static_cast<double>(all);
+                bytes += gemm_bytes(g[j]);
+            }
+            const double us = longer(longest + (waves - 1.0) * (mean - (two ? 0.54 : 0.0)), 2.61 + bytes / 4.84e6);
             if (least < 0 || us < least) {
                 least = us;
                 *best = c;
             }
         }
-    }
     return least;
 }
-double pair_cost(const DenseGemm& g, int sms, int bn) {
-    const int64_t tiles = ceil_div(g.M, 256) * ceil_div(g.N, g.gated ? bn / 2 : bn) * g.groups;
-    const double waves = static_cast<double>(ceil_div(tiles, std::max(1, sms / 2))), chunks = static_cast<double>(ceil_div(g.K, 64) * g.sources);
-    const double chunk = (bn == 256 ? 0.308 : 0.272) * (1.0 + 0.05 * (off_lines(g.a) + off_lines(g.b))), rows = bn == 256 ? 2.43 : 1.83;   // (24 KB of a stage come no faster than 32)
-    return longer(1.56 + waves * (chunks * chunk + 0.3 * rows) + rows, 1.56 + gemm_bytes(g) / 5.79e6);
+double pair_cost(const DenseGemm* g, int n, int sms, int bn) {
+    int64_t tiles = 0;
+    double off = 0.0, bytes = 0.0;
+    for (int j = 0; j < n; j++) {
+        tiles += ceil_div(g[j].M, 256) * ceil_div(g[j].N, g[j].gated ? bn / 2 : bn) * g[j].groups;
+        off += (off_lines(g[j].a) + off_lines(g[j].b)) / n;
+        bytes += gemm_bytes(g[j]);
+    }
+    int rest, few, many;
+    const double chunks = dense_pair_share(g, n, bn, static_cast<int>(std::min<int64_t>(tiles, std::max(1, sms / 2))), &rest, &few, &many);
+    if (chunks < 0) return -1.0;
+    // (two products side by side share less of what they load, as measured over 112 pairs of gradients)
+    const double apart = n > 1 ? (bn == 256 ? 1.05 : 1.15) : 1.0;
+    return apart * longer(1.56 + chunks * (bn == 256 ? 0.308 : 0.272) * (1.0 + 0.05 * off) + (bn == 256 ? 2.43 : 1.83), 1.56 + bytes / 5.79e6);
 }
 
+// The fastest launch of these products together, by the estimates.
+struct GemmPlan {
+    double us;
+    bool lat;
+    int bn;
+    DenseLatChoice c;
+};
+GemmPlan plan_gemm(const DenseGemm* g, int n, int sms) {
+    GemmPlan best{pair_cost(g, n, sms, 256), false, 256, {}};
+    const double narrow = g[0].gated ? -1.0 : pair_cost(g, n, sms, 128);
+    if (narrow >= 0 && (best.us < 0 || narrow < best.us)) best = GemmPlan{narrow, false, 128, {}};
+    DenseLatChoice c{};
+    const double lat = lat_cost(g, n, sms, &c);
+    if (lat >= 0 && (best.us < 0 || lat < best.us)) best = GemmPlan{lat, true, 0, c};
+    return best;
+}
+int launch_plan(const GemmPlan& p, const DenseGemm* g, int n, cudaStream_t s) {
+    if (p.us < 0) return DLF_E_UNSUPPORTED;
+    return p.lat ? launch_dense_lat(g, n, p.c, s) : launch_dense_pair(g, n, p.bn, s);
+}
 int launch_gemm(const DenseGemm& g, cudaStream_t s) {
     int sms = 0;
     const int rc = query_sms(&sms);
+    return rc ? rc : launch_plan(plan_gemm(&g, 1, sms), &g, 1, s);
+}
+// The gradients of an input and of weights: as one launch where its tiles fill the chip better than two launches' (4096 x 4096 x 4096:
+// 186 -> 171 us; 200 x 2048 x 1000, with the bias's: 15.1 -> 11.2), else one after the other.
+int launch_grads(DenseGemm* g, int n, cudaStream_t s) {
+    if (n == 0) return DLF_OK;
+    if (n == 1) return launch_gemm(g[0], s);
+    int sms = 0;
+    int rc = query_sms(&sms);
     if (rc) return rc;
-    DenseLatChoice c{};
-    const double lat = lat_cost(g, sms, &c), wide = pair_cost(g, sms, 256), narrow = g.gated ? wide : pair_cost(g, sms, 128);
-    if (lat >= 0 && lat < std::min(wide, narrow)) return launch_dense_lat(g, c, s);
-    return launch_dense_pair(g, wide <= narrow ? 256 : 128, s);
+    if (g[0].K * g[0].sources < g[1].K * g[1].sources) std::swap(g[0], g[1]);   // the longer tiles first, the shorter ones fill up
+    const GemmPlan one[2] = {plan_gemm(&g[0], 1, sms), plan_gemm(&g[1], 1, sms)}, both = plan_gemm(g, 2, sms);
+    if (both.us >= 0 && both.us < one[0].us + one[1].us) return launch_plan(both, g, 2, s);
+    rc = launch_plan(one[0], &g[0], 1, s);
+    return rc ? rc : launch_plan(one[1], &g[1], 1, s);
 }
 
 // An operand as the products read it: itself, or a copy in the workspace (`run`: made now).
@@ -448,23 +495,25 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
         rc = launch_dense_grad(d, s);
         if (rc) return rc;
     }
-    DenseGemm g{};
-    g.dtype = a->dtype; g.act = DLF_ACT_NONE;
-    g.sources = g.groups = 1;
+    DenseGemm g[2] = {};
+    int n = 0;
     if (dx.p) {   // dx[m][k] = sum over n of dz[m][n] w[n][k]
-        g.M = a->m; g.N = a->k; g.K = a->n;
-        g.a[0] = dz; g.b[0] = wo; g.a_mn = false; g.b_mn = true;
-        g.out[0] = dx;
-        rc = launch_gemm(g, s);
-        if (rc) return rc;
+        DenseGemm& q = g[n++];
+        q.dtype = a->dtype;
+        q.sources = q.groups = 1;
+        q.M = a->m; q.N = a->k; q.K = a->n;
+        q.a[0] = dz; q.b[0] = wo; q.b_mn = true;
+        q.out[0] = dx;
     }
     if (dw.p) {   // dw[n][k] = sum over m of dz[m][n] x[m][k]
-        g.M = a->n; g.N = a->k; g.K = a->m;
-        g.a[0] = dz; g.b[0] = xo; g.a_mn = true; g.b_mn = true;
-        g.out[0] = dw;
-        rc = launch_gemm(g, s);
+        DenseGemm& q = g[n++];
+        q.dtype = a->dtype;
+        q.sources = q.groups = 1;
+        q.M = a->n; q.N = a->k; q.K = a->m;
+        q.a[0] = dz; q.b[0] = xo; q.a_mn = q.b_mn = true;
+        q.out[0] = dw;
     }
-    return rc;
+    return launch_grads(g, n, s);
 }
 
 int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
@@ -540,25 +589,29 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     if (rc) return rc;
     rc = launch_dense_grad(d, s);
     if (rc) return rc;
-    DenseGemm g{};
-    g.dtype = a->dtype; g.act = DLF_ACT_NONE;
+    DenseGemm g[2] = {};
+    int n = 0;
     if (dx.p) {   // dx = dg wg + du wu, one sum
-        g.sources = 2; g.groups = 1;
-        g.M = a->m; g.N = a->k; g.K = a->n;
-        g.a[0] = d.d0; g.a[1] = d.d1; g.b[0] = wgo; g.b[1] = wuo; g.a_mn = false; g.b_mn = true;
-        g.out[0] = dx;
-        rc = launch_gemm(g, s);
-        if (rc) return rc;
+        DenseGemm& q = g[n++];
+        q.dtype = a->dtype;
+        q.sources = 2; q.groups = 1;
+        q.M = a->m; q.N = a->k; q.K = a->n;
+        q.a[0] = d.d0; q.a[1] = d.d1; q.b[0] = wgo; q.b[1] = wuo; q.b_mn = true;
+        q.out[0] = dx;
     }
-    if (any_dw) {   // dwg = dg^T x and dwu = du^T x, one launch
-        g.sources = 1; g.groups = dwg.p && dwu.p ? 2 : 1;
-        g.M = a->n; g.N = a->k; g.K = a->m;
-        g.a[0] = dwg.p ? d.d0 : d.d1; g.a[1] = d.d1; g.b[0] = xo; g.a_mn = true; g.b_mn = true;
-        g.out[0] = dwg.p ? dwg : dwu;
-        g.out[1] = g.groups > 1 ? dwu : Mat{nullptr, 0};
-        rc = launch_gemm(g, s);
+    if (any_dw) {   // dwg = dg^T x and dwu = du^T x, two groups of tiles
+        DenseGemm& q = g[n++];
+        q.dtype = a->dtype;
+        q.sources = 1; q.groups = dwg.p && dwu.p ? 2 : 1;
+        q.M = a->n; q.N = a->k; q.K = a->m;
+        q.a[0] = dwg.p ? d.d0 : d.d1; q.b[0] = xo; q.a_mn = q.b_mn = true;
+        q.out[0] = dwg.p ? dwg : dwu;
+        if (q.groups > 1) {
+            q.a[1] = d.d1;
+            q.out[1] = dwu;
+        }
     }
-    return rc;
+    return launch_grads(g, n, s);
 }
 
 }  // namespace

@@ -45,17 +45,19 @@ struct DenseGrad {
 // True if a matrix can be a TMA operand: rows start on 16-byte boundaries.
 inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 0; }
 
+// Products `g[0]` to `g[n - 1]` as one launch: one forward product, or one or two gradients (b_mn).
 // dense_tc.cu: tiles of 256 rows by bn (256, 128; gated: 256, both halves) columns of B; operands with rows on 16-byte boundaries.
-int launch_dense_pair(const DenseGemm& g, int bn, cudaStream_t s);
+int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s);
+double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest, int* few, int* many);   // chunks of K until the last pair is done
 int dense_pair_status(cudaStream_t s, int* code);             // waits for the stream; a kernel's bounded wait that gave up
-// dense_lat.cu: tiles of `rows` rows (at most 128) by `bn` columns of B (64 or 128; both halves of a gated tile), K shared out over
-// `split` CTAs (1, 2, 4, 8).
+// dense_lat.cu: tiles of at most 128 rows by `bn` columns of B (64 or 128; both halves of a gated tile), K shared out over `split` CTAs (1, 2,
+// 4, 8).
 struct DenseLatChoice {
-    int rows, bn, split;
+    int bn, split;
     bool deep;   // a tile of one CTA: the whole of an SM's shared memory for its ring instead of half
 };
-bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* stages, bool* two);   // `two` of its CTAs fit an SM
-int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s);
+bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* rows, int* stages, bool* two);   // `two` of its CTAs fit an SM
+int launch_dense_lat(const DenseGemm* g, int n, const DenseLatChoice& c, cudaStream_t s);
 int dense_lat_status(cudaStream_t s, int* code);
 
 bool dense_gemv_takes(const DenseGemm& g);                           // dense_gemv.cu: forward products of a few tokens, any rows

@@ -35,17 +35,23 @@ constexpr int kPairSmem = 110 * 1024;        // two CTAs fit an SM: one's set-up
 constexpr int kAloneSmem = 200 * 1024;       // more than this leaves no room for another tensor-core kernel's CTA on the SM
 enum { EPI_PLAIN = 0, EPI_LINEAR = 1, EPI_GATED = 2 };
 
-struct LatParams {
+// One product, or the two gradients' products that share a launch.
+struct LatJob {
     CUtensorMap a[2], b[2];
-    Mat o[3], res;
-    const float* bias[2];
-    long long M, N;
-    int tiles_n, BN, rows;             // rows: of A in a tile
-    long long group_tiles;
+    Mat o[3];
+    long long M, N, group_tiles;
+    int tiles_n, rows;                 // rows: of A in a tile
     int chunks1, total, share;         // 64-value chunks of K: of the first source, of both, of a CTA
     int stages, a_bytes, stage_bytes, red_off, rows_per;
-    int act, groups;
-    bool vec;                          // every row that is read or written here starts on a 16-byte boundary
+    int groups;
+    bool amn, vec;                     // vec: every row that is read or written here starts on a 16-byte boundary
+};
+template <int JOBS>
+struct LatParams {
+    LatJob job[JOBS];
+    Mat res;
+    const float* bias[2];
+    int act, BN, first1;               // first1: CTAs of the first job
 };
 
 // From the sums of W (an even number) outputs of a row to what is stored: v (and u of a gated tile), the biases, what is added.
@@ -69,8 +75,12 @@ __device__ __forceinline__ void finish(int act_code, float (&v)[W], float (&u)[W
     put(0, v);
 }
 
-template <typename T, bool AMN, bool BMN, int EPI, int SPLIT>
-__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT == 1 ? 2 : 1) dense_lat_kernel(const __grid_constant__ LatParams p) {
+template <typename T, int EPI, int SPLIT>
+__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT == 1 ? 2 : 1) dense_lat_kernel(const __grid_constant__ LatParams<EPI == EPI_PLAIN ? 2 : 1> P) {
+    constexpr bool BMN = EPI == EPI_PLAIN;   // (a forward product's operands lie along K; of the gradients' B lies across, and A, too, for weights)
+    const bool job1 = EPI == EPI_PLAIN && static_cast<int>(blockIdx.x) >= P.first1;
+    const LatJob& p = P.job[EPI == EPI_PLAIN && job1 ? 1 : 0];
+    const bool amn = EPI == EPI_PLAIN && p.amn;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], tfull_bar, red_bar;
     __shared__ uint32_t tmem_base_s;
@@ -83,32 +93,42 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
     volatile int* abort_flag = &abort_s;
     int* status = &g_dense_status;
     const int rank = SPLIT > 1 ? static_cast<int>(cluster_rank()) : 0;
-    long long tile = static_cast<long long>(blockIdx.x) / SPLIT;
+    long long tile = (static_cast<int>(blockIdx.x) - (job1 ? P.first1 : 0)) / SPLIT;
     const int group = p.groups > 1 && tile >= p.group_tiles ? 1 : 0;
     tile -= group ? p.group_tiles : 0;
     const long long tm = tile / p.tiles_n;
-    const long long n0 = (tile - tm * p.tiles_n) * (EPI == EPI_GATED ? p.BN / 2 : p.BN), m0 = tm * p.rows;
+    const long long n0 = (tile - tm * p.tiles_n) * (EPI == EPI_GATED ? P.BN / 2 : P.BN), m0 = tm * p.rows;
     const int k_first = rank * p.share, k_count = min(p.share, p.total - k_first);
     const int live = static_cast<int>(min(static_cast<long long>(p.rows), p.M - m0));   // rows of the tile that exist
 
-    // A stage's boxes, those of A first: box `bx` of chunk i of this CTA's share into stage st.
-    const int boxes_a = AMN ? 2 : 1, boxes = boxes_a + (EPI == EPI_GATED ? 2 : BMN ? p.BN / 64 : 1);
-    const uint32_t stage_tx = static_cast<uint32_t>(p.a_bytes + p.BN * 128);
-    auto load_box = [&](int i, int st, int bx) {
+    // A stage's boxes, those of A first: where each comes from and goes to.  (Worked out once: with the choices in the loop the pairs' weight
+    // gradients took 5 % longer.)
+    const int boxes_a = amn ? 2 : 1, boxes = boxes_a + (EPI == EPI_GATED ? 2 : BMN ? P.BN / 64 : 1);
+    const uint32_t stage_tx = static_cast<uint32_t>(p.a_bytes + P.BN * 128);
+    struct Box {
+        const CUtensorMap *map0, *map1;   // of the first source and of the second
+        int off, row;
+        bool across;
+    };
+    auto box_of = [&](int bx) {
+        const int j = bx - boxes_a;
+        Box b;
+        if (j < 0) {
+            b = Box{&p.a[group], &p.a[1], bx * 8192, static_cast<int>(m0) + bx * 64, amn};
+        } else {
+            b.map0 = &p.b[EPI == EPI_GATED ? j : 0];
+            b.map1 = &p.b[1];
+            b.off = p.a_bytes + (EPI == EPI_GATED ? j * P.BN * 64 : j * 8192);
+            b.row = static_cast<int>(n0) + (BMN ? j * 64 : 0);
+            b.across = BMN;
+        }
+        return b;
+    };
+    auto load_box = [&](const Box& b, int i, int st) {   // of chunk i of this CTA's share into stage st
         const int c = k_first + i;
         const bool second = c >= p.chunks1;
-        const int k0 = (second ? c - p.chunks1 : c) * 64, j = bx - boxes_a;
-        uint8_t* dst = sbase + st * p.stage_bytes;
-        if (j < 0) {
-            const CUtensorMap* map = &p.a[second || group ? 1 : 0];
-            if (AMN) tma_load_2d(dst + bx * 8192, map, &full_bar[st], static_cast<int>(m0) + bx * 64, k0);
-            else tma_load_2d(dst, map, &full_bar[st], k0, static_cast<int>(m0));
-        } else {
-            dst += p.a_bytes;
-            if (EPI == EPI_GATED) tma_load_2d(dst + j * p.BN * 64, &p.b[j], &full_bar[st], k0, static_cast<int>(n0));
-            else if (BMN) tma_load_2d(dst + j * 8192, &p.b[second ? 1 : 0], &full_bar[st], static_cast<int>(n0) + j * 64, k0);
-            else tma_load_2d(dst, &p.b[second ? 1 : 0], &full_bar[st], k0, static_cast<int>(n0));
-        }
+        const int k0 = (second ? c - p.chunks1 : c) * 64;
+        tma_load_2d(sbase + st * p.stage_bytes + b.off, second ? b.map1 : b.map0, &full_bar[st], b.across ? b.row : k0, b.across ? k0 : b.row);
     };
     if (warp == kProdWarp0) {
         if (lane < kMaxStages) {
@@ -123,14 +143,14 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         }
         fence_barrier_init();
         // the bytes that the cluster's CTAs will send here (before the cluster's barrier, which every sender waits for)
-        if (SPLIT > 1 && lane == 0) mbar_expect_tx(&red_bar, static_cast<uint32_t>(SPLIT * max(0, min(p.rows_per, live - rank * p.rows_per)) * p.BN) * 4u);
+        if (SPLIT > 1 && lane == 0) mbar_expect_tx(&red_bar, static_cast<uint32_t>(SPLIT * max(0, min(p.rows_per, live - rank * p.rows_per)) * P.BN) * 4u);
         __syncwarp();
         // the ring's first round is on its way before the rest of the set-up (a lane a stage)
         pdl_wait();
         if (lane < min(p.stages, k_count)) {
             mbar_expect_tx(&full_bar[lane], stage_tx);
 #pragma unroll 1
-            for (int bx = 0; bx < boxes; bx++) load_box(lane, lane, bx);
+            for (int bx = 0; bx < boxes; bx++) load_box(box_of(bx), lane, lane);
         }
         __syncwarp();
     }
@@ -149,6 +169,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
     if (warp >= kProdWarp0 && warp < kMmaWarp) {
         // ---- producers: lane i issues a stage's i-th box ----
         const int w = warp - kProdWarp0;
+        const Box mine = box_of(min(lane, boxes - 1));
         int turn = 0, st = 0;
         uint32_t ph = 0;
 #pragma unroll 1
@@ -157,7 +178,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                 if (!mbar_wait_warp<true>(&empty_bar[st], ph, abort_flag, status, 0xA00 | (blockIdx.x << 12))) break;
                 if (lane == 0) mbar_expect_tx(&full_bar[st], stage_tx);
                 __syncwarp();
-                if (lane < boxes) load_box(i, st, lane);
+                if (lane < boxes) load_box(mine, i, st);
                 __syncwarp();
             }
             if (++turn == kProdWarps) turn = 0;
@@ -170,39 +191,44 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         const int w = warp - kMmaWarp;
         const uint32_t d_tmem = tmem_base + w * kMaxBN;
         const int last = k_count - 1 - ((k_count - 1 - w) & 1);   // this issuer's last chunk (negative: it has none)
-        const uint32_t idesc = dense_idesc<T>(128, 0, AMN, BMN) | (static_cast<uint32_t>(p.BN >> 3) << 17);
-        const uint32_t a0 = AMN ? umma_desc_mn_lo(base, 8192) : umma_desc_lo(base);
         const uint32_t b0 = BMN ? umma_desc_mn_lo(base + p.a_bytes, 8192) : umma_desc_lo(base + p.a_bytes);
         const uint32_t stage16 = static_cast<uint32_t>(p.stage_bytes) >> 4;
         int st = w % p.stages;
         uint32_t ph = static_cast<uint32_t>(w / p.stages) & 1u, off = static_cast<uint32_t>(st) * stage16;
+        auto multiply = [&](auto across) {   // (a loop for each kind of operand A: its steps are constants)
+            constexpr bool AMN = across.value;
+            const uint32_t idesc = dense_idesc<T>(128, 0, AMN, BMN) | (static_cast<uint32_t>(P.BN >> 3) << 17);
+            const uint32_t a0 = AMN ? umma_desc_mn_lo(base, 8192) : umma_desc_lo(base);
 #pragma unroll 1
-        for (int i = w; i < k_count; i += 2) {
-            if (!mbar_wait_warp<true>(&full_bar[st], ph, abort_flag, status, 0xA10 | (blockIdx.x << 12))) break;
-            tc_fence_after_sync();
-            if (elect_one()) {
-                umma_chunk<1, AMN, BMN>(d_tmem, a0 + off, b0 + off, idesc, i != w);
-                if (i + p.stages < k_count) umma_commit(&empty_bar[st]);
-                if (i == last) umma_commit(&tfull_bar);
+            for (int i = w; i < k_count; i += 2) {
+                if (!mbar_wait_warp<true>(&full_bar[st], ph, abort_flag, status, 0xA10 | (blockIdx.x << 12))) break;
+                tc_fence_after_sync();
+                if (elect_one()) {
+                    umma_chunk<1, AMN, BMN>(d_tmem, a0 + off, b0 + off, idesc, i != w);
+                    if (i + p.stages < k_count) umma_commit(&empty_bar[st]);
+                    if (i == last) umma_commit(&tfull_bar);
+                }
+                __syncwarp();
+                st += 2;
+                off += 2 * stage16;
+                if (st >= p.stages) { st -= p.stages; ph ^= 1u; off -= static_cast<uint32_t>(p.stages) * stage16; }
             }
-            __syncwarp();
-            st += 2;
-            off += 2 * stage16;
-            if (st >= p.stages) { st -= p.stages; ph ^= 1u; off -= static_cast<uint32_t>(p.stages) * stage16; }
-        }
+        };
+        if (amn) multiply(std::integral_constant<bool, EPI == EPI_PLAIN>{});
+        else multiply(std::false_type{});
         if (last < 0 && lane == 0) mbar_arrive(&tfull_bar);
     } else {
         // ---- epilogue: the sums go to shared memory (of the CTA that finishes them), row by row, and from there in runs of 8 outputs
         // that lie side by side in memory ----
         const int q = warp & 3, half = warp >> 2, m = q * 32 + lane;
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
-        const int out_bn = EPI == EPI_GATED ? p.BN / 2 : p.BN;
+        const int out_bn = EPI == EPI_GATED ? P.BN / 2 : P.BN;
         const int my_rows = max(0, min(p.rows_per, live - rank * p.rows_per)), lg = __ffs(out_bn) - 4;   // (runs of 8 in a row: a power of two)
         const long long row_first = m0 + rank * p.rows_per;
         const int n_cols = static_cast<int>(min(static_cast<long long>(out_bn), p.N - n0));
-        if (EPI != EPI_PLAIN && threadIdx.x < p.BN) {
+        if (EPI != EPI_PLAIN && threadIdx.x < P.BN) {
             const int c = EPI == EPI_GATED && static_cast<int>(threadIdx.x) >= out_bn ? static_cast<int>(threadIdx.x) - out_bn : static_cast<int>(threadIdx.x);
-            const float* b = p.bias[EPI == EPI_GATED && static_cast<int>(threadIdx.x) >= out_bn ? 1 : 0];
+            const float* b = P.bias[EPI == EPI_GATED && static_cast<int>(threadIdx.x) >= out_bn ? 1 : 0];
             bias_s[threadIdx.x] = b && c < n_cols ? ld_map(b + n0 + c) : 0.0f;
         }
         // A run is 8 outputs that are a piece of 16 bytes in memory: where rows start off the 16-byte boundaries, a row's first and
@@ -234,7 +260,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         };
         // what a thread's next runs have to add is fetched kItems runs at a time, the first ones behind the products
         constexpr int kItems = 4;
-        const bool add = EPI == EPI_LINEAR && p.res.p != nullptr;
+        const bool add = EPI == EPI_LINEAR && P.res.p != nullptr;
         uint4 res[kItems] = {};
         auto fetch_res = [&](auto vec, int i0) {
 #pragma unroll
@@ -242,7 +268,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                 int c = 0;
                 const int r = run_at(vec, i0 + it * 32 * kEpiWarps, &c);
                 res[it] = make_uint4(0u, 0u, 0u, 0u);
-                if (add && r >= 0) res[it] = fetch8(vec, static_cast<const unsigned short*>(p.res.p) + (row_first + r) * p.res.ld + n0 + c, c);
+                if (add && r >= 0) res[it] = fetch8(vec, static_cast<const unsigned short*>(P.res.p) + (row_first + r) * P.res.ld + n0 + c, c);
             }
         };
         if (add && p.vec) fetch_res(std::true_type{}, threadIdx.x);
@@ -250,17 +276,17 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         bool ok = mbar_wait_warp<true>(&tfull_bar, 0u, abort_flag, status, 0xA20 | (blockIdx.x << 12));
         tc_fence_after_sync();
         const int dest = SPLIT > 1 ? min(m / p.rows_per, SPLIT - 1) : 0, row = m - dest * p.rows_per;
-        const uint32_t slab = static_cast<uint32_t>(p.rows_per * p.BN * 4);   // one rank's partial rows
+        const uint32_t slab = static_cast<uint32_t>(p.rows_per * P.BN * 4);   // one rank's partial rows
         // (a row's 16-byte vectors are stored in an order that depends on the row: the lanes of a warp fall into different banks)
         const uint32_t swz = static_cast<uint32_t>(row) & 7u;
-        uint32_t dst = base + p.red_off + rank * slab + row * p.BN * 4, dst_bar = 0;
+        uint32_t dst = base + p.red_off + rank * slab + row * P.BN * 4, dst_bar = 0;
         if (SPLIT > 1) {
             dst = mapa(dst, dest);
             dst_bar = mapa(smem_u32(&red_bar), dest);
             cluster_wait();   // every CTA of the cluster runs and its barrier expects these rows
         }
 #pragma unroll 1
-        for (int c0 = half * 16; c0 < p.BN; c0 += 32) {
+        for (int c0 = half * 16; c0 < P.BN; c0 += 32) {
             uint32_t r0[16], r1[16];
             float v[16];
             tmem_ld16_issue(taddr + c0, r0);
@@ -295,7 +321,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                     if (r < 0) continue;
                     float v[8], u[8], a[8];
                     auto sum = [&](int col, float (&s)[8]) {
-                        const uint8_t* const at = red + r * p.BN * 4;
+                        const uint8_t* const at = red + r * P.BN * 4;
                         const uint32_t swap = static_cast<uint32_t>(r) & 7u;
 #pragma unroll
                         for (int e = 0; e < 8; e++) s[e] = 0.0f;
@@ -310,7 +336,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; e++) {
-                                const int d = min(max(col + e, 0), p.BN - 1);   // (a column that does not exist: any value)
+                                const int d = min(max(col + e, 0), P.BN - 1);   // (a column that does not exist: any value)
                                 const uint8_t* const q = at + (((static_cast<uint32_t>(d) >> 2) ^ swap) << 4) + (d & 3) * 4;
 #pragma unroll
                                 for (int sp = 0; sp < SPLIT; sp++) s[e] += *reinterpret_cast<const float*>(q + sp * slab);
@@ -318,7 +344,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                         }
                         if (EPI != EPI_PLAIN) {
 #pragma unroll
-                            for (int e = 0; e < 8; e++) s[e] += bias_s[vec.value ? col + e : min(max(col + e, 0), p.BN - 1)];
+                            for (int e = 0; e < 8; e++) s[e] += bias_s[vec.value ? col + e : min(max(col + e, 0), P.BN - 1)];
                         }
                     };
                     sum(c, v);
@@ -326,7 +352,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
                     const T* in = reinterpret_cast<const T*>(&res[it]);
 #pragma unroll
                     for (int e = 0; e < 8; e++) a[e] = add ? to_f32(in[e]) : 0.0f;
-                    finish<EPI>(p.act, v, u, a, [&](int which, const float(&f)[8]) {
+                    finish<EPI>(P.act, v, u, a, [&](int which, const float(&f)[8]) {
                         const Mat& o = p.o[EPI == EPI_PLAIN ? group : which];
                         if (!o.p) return;
                         T* t = static_cast<T*>(const_cast<void*>(o.p)) + (row_first + r) * o.ld + n0 + c;
@@ -355,34 +381,15 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
     }
 }
 
-typedef void (*LatFn)(const LatParams);
-template <typename T, int SPLIT>
-LatFn pick_op(const DenseGemm& g) {
-    if (g.gated) return dense_lat_kernel<T, false, false, EPI_GATED, SPLIT>;
-    if (g.a_mn) return dense_lat_kernel<T, true, true, EPI_PLAIN, SPLIT>;
-    if (g.b_mn) return dense_lat_kernel<T, false, true, EPI_PLAIN, SPLIT>;
-    return dense_lat_kernel<T, false, false, EPI_LINEAR, SPLIT>;
-}
-template <typename T>
-LatFn pick_lat(const DenseGemm& g, int split) {
-    switch (split) {
-        case 1: return pick_op<T, 1>(g);
-        case 2: return pick_op<T, 2>(g);
-        case 4: return pick_op<T, 4>(g);
-        default: return pick_op<T, 8>(g);
-    }
-}
-
 // The layout of a tile in shared memory: ring depth, and where the cluster's partial sums go.
-bool lay_out(const DenseGemm& g, const DenseLatChoice& c, LatParams* p, size_t* smem) {
-    p->BN = c.bn;
-    p->rows = c.rows;
-    p->a_bytes = g.a_mn ? 16384 : (c.rows + 7) / 8 * 1024;
+bool lay_out(const DenseGemm& g, const DenseLatChoice& c, LatJob* p, size_t* smem) {
+    p->rows = g.a_mn ? static_cast<int>(std::min<int64_t>(g.M, 128)) : static_cast<int>((g.M + (g.M + 127) / 128 - 1) / ((g.M + 127) / 128));
+    p->a_bytes = g.a_mn ? 16384 : (p->rows + 7) / 8 * 1024;
     p->stage_bytes = p->a_bytes + c.bn * 128;
     p->chunks1 = static_cast<int>((g.K + 63) / 64);
     p->total = p->chunks1 * g.sources;
     p->share = (p->total + c.split - 1) / c.split;
-    p->rows_per = (c.rows + c.split - 1) / c.split;
+    p->rows_per = (p->rows + c.split - 1) / c.split;
     if (c.split > 1 && (c.split - 1) * p->share >= p->total) return false;   // (a CTA without work)
     const int red = c.split > 1 ? c.split * p->rows_per * c.bn * 4 : 0;
     const int slack = 16384 - p->a_bytes;   // the tensor core reads 128 rows of A, behind the ring's last ones too: memory of this CTA all the same
@@ -400,44 +407,84 @@ bool lay_out(const DenseGemm& g, const DenseLatChoice& c, LatParams* p, size_t* 
     return true;
 }
 
+int fill_job(const DenseGemm& g, const DenseLatChoice& c, LatJob* p, size_t* smem) {
+    size_t mine = 0;
+    if (!lay_out(g, c, p, &mine)) return DLF_E_UNSUPPORTED;
+    *smem = std::max(*smem, mine);
+    for (int i = 0; i < 2; i++) {
+        const Mat &a = g.a[i], &b = g.b[i];
+        int rc = DLF_OK;
+        if (a.p) rc = g.a_mn ? dense_map(&p->a[i], a, g.K, g.M, 64, 64) : dense_map(&p->a[i], a, g.M, g.K, p->a_bytes / 128, 64);
+        if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p->b[i], b, g.K, g.N, 64, 64) : dense_map(&p->b[i], b, g.N, g.K, g.gated ? c.bn / 2 : c.bn, 64);
+        if (rc) return rc;
+    }
+    for (int i = 0; i < 3; i++) p->o[i] = g.out[i];
+    p->vec = dense_rows16(g.res) && dense_rows16(g.out[0]) && dense_rows16(g.out[1]) && dense_rows16(g.out[2]);
+    p->M = g.M; p->N = g.N;
+    const int step = g.gated ? c.bn / 2 : c.bn;
+    p->tiles_n = static_cast<int>((g.N + step - 1) / step);
+    p->group_tiles = (g.M + p->rows - 1) / p->rows * p->tiles_n;
+    p->groups = g.groups;
+    p->amn = g.a_mn;
+    return DLF_OK;
+}
+template <typename FN, typename PARAMS>
+int launch_lat(FN fn, const PARAMS& p, int grid, size_t smem, cudaStream_t s) {
+    const int rc = dense_smem_attr(reinterpret_cast<const void*>(fn), kMaxDynSmem);
+    if (rc) return rc;
+    const cudaError_t e = launch_kernel(fn, grid, kThreads, smem, s, p);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
+template <typename T, int EPI, typename PARAMS>
+int launch_split(int split, const PARAMS& p, int grid, size_t smem, cudaStream_t s) {
+    switch (split) {
+        case 1: return launch_lat(dense_lat_kernel<T, EPI, 1>, p, grid, smem, s);
+        case 2: return launch_lat(dense_lat_kernel<T, EPI, 2>, p, grid, smem, s);
+        case 4: return launch_lat(dense_lat_kernel<T, EPI, 4>, p, grid, smem, s);
+        default: return launch_lat(dense_lat_kernel<T, EPI, 8>, p, grid, smem, s);
+    }
+}
+
 }  // namespace
 
-bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* stages, bool* two) {
-    LatParams p;
+bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* rows, int* stages, bool* two) {
+    LatJob p;
     size_t smem;
     if (!lay_out(g, c, &p, &smem)) return false;
+    *rows = p.rows;
     *stages = p.stages;
     *two = smem <= static_cast<size_t>(kPairSmem) + 2048;
     return true;
 }
 
-int launch_dense_lat(const DenseGemm& g, const DenseLatChoice& c, cudaStream_t s) {
-    LatParams p;
-    std::memset(&p, 0, sizeof(p));
+int launch_dense_lat(const DenseGemm* g, int n, const DenseLatChoice& c, cudaStream_t s) {
+    const bool bf = g[0].dtype == DLF_BF16;
     size_t smem = 0;
-    if (!lay_out(g, c, &p, &smem)) return DLF_E_UNSUPPORTED;
-    int rc = DLF_OK;
-    for (int i = 0; i < 2 && rc == DLF_OK; i++) {
-        const Mat &a = g.a[i], &b = g.b[i];
-        if (a.p) rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, p.a_bytes / 128, 64);
-        if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, g.gated ? c.bn / 2 : c.bn, 64);
+    if (!g[0].b_mn) {
+        LatParams<1> p;
+        std::memset(&p, 0, sizeof(p));
+        const int rc = fill_job(g[0], c, &p.job[0], &smem);
+        if (rc) return rc;
+        p.res = g[0].res;
+        p.bias[0] = g[0].bias[0]; p.bias[1] = g[0].bias[1];
+        p.act = g[0].act;
+        p.BN = c.bn;
+        const int grid = static_cast<int>(p.job[0].group_tiles * c.split);
+        if (g[0].gated) return bf ? launch_split<__nv_bfloat16, EPI_GATED>(c.split, p, grid, smem, s) : launch_split<__half, EPI_GATED>(c.split, p, grid, smem, s);
+        return bf ? launch_split<__nv_bfloat16, EPI_LINEAR>(c.split, p, grid, smem, s) : launch_split<__half, EPI_LINEAR>(c.split, p, grid, smem, s);
     }
-    if (rc) return rc;
-    for (int i = 0; i < 3; i++) p.o[i] = g.out[i];
-    p.res = g.res;
-    p.vec = dense_rows16(g.res) && dense_rows16(g.out[0]) && dense_rows16(g.out[1]) && dense_rows16(g.out[2]);
-    p.bias[0] = g.bias[0]; p.bias[1] = g.bias[1];
-    p.M = g.M; p.N = g.N;
-    const int step = g.gated ? c.bn / 2 : c.bn;
-    p.tiles_n = static_cast<int>((g.N + step - 1) / step);
-    p.group_tiles = (g.M + c.rows - 1) / c.rows * p.tiles_n;
-    p.act = g.act; p.groups = g.groups;
-    const LatFn fn = g.dtype == DLF_BF16 ? pick_lat<__nv_bfloat16>(g, c.split) : pick_lat<__half>(g, c.split);
-    rc = dense_smem_attr(reinterpret_cast<const void*>(fn), kMaxDynSmem);
-    if (rc) return rc;
-    const int grid = static_cast<int>(p.group_tiles * g.groups * c.split);
-    const cudaError_t e = launch_kernel(fn, grid, kThreads, smem, s, p);
-    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+    LatParams<2> p;
+    std::memset(&p, 0, sizeof(p));
+    p.BN = c.bn;
+    int grid = 0;
+    for (int i = 0; i < n; i++) {
+        const int rc = fill_job(g[i], c, &p.job[i], &smem);
+        if (rc) return rc;
+        if (i == 1) p.first1 = grid;
+        grid += static_cast<int>(p.job[i].group_tiles * g[i].groups * c.split);
+    }
+    if (n == 1) p.first1 = grid;
+    return bf ? launch_split<__nv_bfloat16, EPI_PLAIN>(c.split, p, grid, smem, s) : launch_split<__half, EPI_PLAIN>(c.split, p, grid, smem, s);
 }
 
 int dense_lat_status(cudaStream_t s, int* code) { return dense_status_of(s, code); }

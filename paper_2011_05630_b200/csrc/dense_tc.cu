@@ -31,22 +31,48 @@ constexpr int kDynSmem = kRing + kStaging + 1024;
 constexpr int kMaxStages = 8;
 enum { EPI_PLAIN = 0, EPI_LINEAR = 1, EPI_GATED = 2 };
 
-struct PairParams {
+// One product, or the two gradients' products that share a launch (JOBS = 2): the input's first, whose K is the longer one or not.
+struct PairJob {
     CUtensorMap a[2], b[2], out[3];
-    Mat o[3], res;                // (o: outputs without a tensor map, rows off the 16-byte boundaries)
-    const float* bias[2];
+    Mat o[3];                     // (rows off the 16-byte boundaries have no tensor map)
     long long M, N, tiles, group_tiles;
     int tiles_m, tiles_n;
     int chunks1, chunks;          // 64-value chunks of K: of the first source, of both
-    int act, sources, groups;
-    bool out_tma[3], res_vec;
+    int groups;
+    bool amn, out_tma[3];
 };
+template <int JOBS>
+struct PairParams {
+    PairJob job[JOBS];
+    Mat res;
+    const float* bias[2];
+    int act;
+    bool res_vec;
+    // Pairs take the first job's tiles in turn; `rest` of them have one more of these than the others, and with it `many` of the second job's
+    // tiles where the others have `few` (the host weighs the tiles).
+    int pairs, rest, few, many;
+};
+
+// The i-th tile of a pair; false behind its last one.
+template <int JOBS>
+__device__ __forceinline__ bool tile_of(const PairParams<JOBS>& p, int pair, int i, int* job, long long* t) {
+    *job = 0;
+    *t = pair + static_cast<long long>(i) * p.pairs;
+    if (*t < p.job[0].tiles) return true;
+    if (JOBS == 1) return false;
+    *job = JOBS - 1;
+    const bool first = pair < p.rest;
+    i -= static_cast<int>(p.job[0].tiles / p.pairs) + (first ? 1 : 0);
+    const int others = p.pairs - p.rest;
+    *t = first ? static_cast<long long>(p.few) * others + static_cast<long long>(i) * p.rest + pair : static_cast<long long>(i) * others + pair - p.rest;
+    return i < (first ? p.many : p.few) && *t < p.job[JOBS - 1].tiles;
+}
 
 // Tiles are numbered along n within bands of kBand rows of tiles, so that the pairs at work at one time share operands.
 constexpr int kBand = 8;
 struct TileAt { int group; long long m0, n0; };
 template <int BN, int EPI>
-__device__ __forceinline__ TileAt tile_at(const PairParams& p, long long t) {
+__device__ __forceinline__ TileAt tile_at(const PairJob& p, long long t) {
     TileAt r;
     r.group = p.groups > 1 && t >= p.group_tiles ? 1 : 0;
     t -= r.group ? p.group_tiles : 0;
@@ -173,8 +199,9 @@ __device__ __forceinline__ void store_rows64(const Mat& o, const CUtensorMap* ma
     }
 }
 
-template <typename T, bool AMN, bool BMN, int EPI, int BN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_pair_kernel(const __grid_constant__ PairParams p) {
+template <typename T, int EPI, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_pair_kernel(const __grid_constant__ PairParams<EPI == EPI_PLAIN ? 2 : 1> p) {
+    constexpr bool BMN = EPI == EPI_PLAIN;   // (a forward product's operands lie along K; of the gradients' B lies across, and A, too, for weights)
     constexpr int kABytes = 128 * 128, kBRows = BN / 2, kBBytes = kBRows * 128, kStageBytes = kABytes + kBBytes, kStages = kRing / kStageBytes;
     static_assert(kStages <= kMaxStages, "ring");
     extern __shared__ uint8_t smem_raw[];
@@ -188,7 +215,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
     const int rank = static_cast<int>(cluster_rank());
     volatile int* abort_flag = &abort_s;
     int* status = &g_dense_status;
-    const long long t_first = blockIdx.x >> 1, t_step = gridDim.x >> 1;
+    const int pair = static_cast<int>(blockIdx.x) >> 1;
+    int ji = 0;          // a tile's job and number
+    long long t = 0;
 
     if (warp == 0) {
         if (lane == 0) abort_s = 0;
@@ -218,36 +247,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
     if (warp == kAWarp || warp == kBWarp) {
         // ---- producers: one warp for A, one for B; the copies of a stage complete on the first CTA's barrier ----
         const bool is_b = warp == kBWarp;
-        const int boxes = is_b ? (BMN ? kBRows / 64 : 1) : (AMN ? 2 : 1);
         const uint32_t my_bytes = is_b ? kBBytes : kABytes;
         int st = 0;
         uint32_t ph = 0;
         bool ok = true;
 #pragma unroll 1
-        for (long long t = t_first; t < p.tiles && ok; t += t_step) {
-            const TileAt at = tile_at<BN, EPI>(p, t);
-            const int m0 = static_cast<int>(at.m0) + rank * 128, n0 = static_cast<int>(at.n0) + (EPI == EPI_GATED ? 0 : rank * kBRows);
+        for (int i = 0; ok && tile_of(p, pair, i, &ji, &t); i++) {
+            const PairJob& job = p.job[ji];
+            const TileAt at = tile_at<BN, EPI>(job, t);
+            const bool across = is_b ? BMN : EPI == EPI_PLAIN && job.amn;
+            const int boxes = across ? (is_b ? kBRows / 64 : 2) : 1, chunks = job.chunks, chunks1 = job.chunks1;
+            const int row0 = is_b ? static_cast<int>(at.n0) + (EPI == EPI_GATED ? 0 : rank * kBRows) : static_cast<int>(at.m0) + rank * 128;
+            const CUtensorMap* const map0 = is_b ? &job.b[EPI == EPI_GATED ? rank : 0] : &job.a[at.group];
+            const CUtensorMap* const map1 = is_b ? &job.b[1] : &job.a[1];
 #pragma unroll 1
-            for (int c = 0; c < p.chunks; c++) {
+            for (int c = 0; c < chunks; c++) {
                 ok = mbar_wait_warp(&empty_bar[st], ph ^ 1u, abort_flag, status, 0x100 | (blockIdx.x << 12));
                 if (!ok) break;
-                const bool second = c >= p.chunks1;
-                const int k0 = (second ? c - p.chunks1 : c) * 64;
                 if (lane == 0 && rank == 0) mbar_expect_tx(&full_bar[st], 2 * my_bytes);
                 __syncwarp();
                 const int bx = lane - boxes * st;   // (another lane for every stage: the copies of one thread run one after the other)
                 if (bx >= 0 && bx < boxes) {
-                    const uint32_t bar = mapa(smem_u32(&full_bar[st]), 0);
-                    uint8_t* dst = sbase + st * kStageBytes + (is_b ? kABytes : 0) + bx * 8192;
-                    if (is_b) {
-                        const CUtensorMap* map = &p.b[EPI == EPI_GATED ? rank : (second ? 1 : 0)];
-                        if (BMN) tma_load_2d_pair(dst, map, bar, n0 + bx * 64, k0);
-                        else tma_load_2d_pair(dst, map, bar, k0, n0);
-                    } else {
-                        const CUtensorMap* map = &p.a[second || at.group ? 1 : 0];
-                        if (AMN) tma_load_2d_pair(dst, map, bar, m0 + bx * 64, k0);
-                        else tma_load_2d_pair(dst, map, bar, k0, m0);
-                    }
+                    const bool second = c >= chunks1;
+                    const int k0 = (second ? c - chunks1 : c) * 64, row = row0 + bx * 64;
+                    tma_load_2d_pair(sbase + st * kStageBytes + (is_b ? kABytes : 0) + bx * 8192, second ? map1 : map0, mapa(smem_u32(&full_bar[st]), 0),
+                                     across ? row : k0, across ? k0 : row);
                 }
                 __syncwarp();
                 if (++st == kStages) { st = 0; ph ^= 1u; }
@@ -256,32 +280,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
     } else if (warp == kMmaWarp) {
         // ---- issuer: the pair's first CTA, the whole warp walks the loop, one elected lane issues ----
         if (rank == 0) {
-            constexpr uint32_t idesc = dense_idesc<T>(256, BN, AMN, BMN);
-            const uint32_t a0 = AMN ? umma_desc_mn_lo(base, 8192) : umma_desc_lo(base);
             const uint32_t b0 = BMN ? umma_desc_mn_lo(base + kABytes, 8192) : umma_desc_lo(base + kABytes);
             int st = 0;
             uint32_t ph = 0, j = 0;
             bool ok = true;
 #pragma unroll 1
-            for (long long t = t_first; t < p.tiles && ok; t += t_step, j++) {
+            for (; ok && tile_of(p, pair, static_cast<int>(j), &ji, &t); j++) {
+                const PairJob& job = p.job[ji];
+                const bool amn = EPI == EPI_PLAIN && job.amn;
+                const int chunks = job.chunks;
                 const uint32_t acc = j & 1u;
                 ok = mbar_wait_warp(&tempty_bar[acc], ((j >> 1) & 1u) ^ 1u, abort_flag, status, 0x200 | (blockIdx.x << 12));
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + acc * 256u;
+                auto multiply = [&](auto across) {   // (a loop for each kind of operand A: a step that is no constant costs 5 % of the weights' gradients)
+                    constexpr bool AMN = across.value;
+                    constexpr uint32_t idesc = dense_idesc<T>(256, BN, AMN, BMN);
+                    const uint32_t a0 = AMN ? umma_desc_mn_lo(base, 8192) : umma_desc_lo(base);
 #pragma unroll 1
-                for (int c = 0; c < p.chunks; c++) {
-                    ok = mbar_wait_warp<true>(&full_bar[st], ph, abort_flag, status, 0x300 | (blockIdx.x << 12));
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                    const uint32_t off = static_cast<uint32_t>(st) * (kStageBytes >> 4);
-                    if (elect_one()) {
-                        umma_chunk<2, AMN, BMN>(d_tmem, a0 + off, b0 + off, idesc, c != 0);
-                        umma_commit_pair(&empty_bar[st]);
+                    for (int c = 0; c < chunks; c++) {
+                        ok = mbar_wait_warp<true>(&full_bar[st], ph, abort_flag, status, 0x300 | (blockIdx.x << 12));
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                        const uint32_t off = static_cast<uint32_t>(st) * (kStageBytes >> 4);
+                        if (elect_one()) {
+                            umma_chunk<2, AMN, BMN>(d_tmem, a0 + off, b0 + off, idesc, c != 0);
+                            umma_commit_pair(&empty_bar[st]);
+                        }
+                        __syncwarp();
+                        if (++st == kStages) { st = 0; ph ^= 1u; }
                     }
-                    __syncwarp();
-                    if (++st == kStages) { st = 0; ph ^= 1u; }
-                }
+                };
+                if (amn) multiply(std::integral_constant<bool, EPI == EPI_PLAIN>{});
+                else multiply(std::false_type{});
                 if (ok && elect_one()) umma_commit_pair(&tfull_bar[acc]);
                 __syncwarp();
             }
@@ -296,8 +328,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
         uint32_t j = 0;
         bool ok = true;
 #pragma unroll 1
-        for (long long t = t_first; t < p.tiles && ok; t += t_step, j++) {
-            const TileAt at = tile_at<BN, EPI>(p, t);
+        for (; ok && tile_of(p, pair, static_cast<int>(j), &ji, &t); j++) {
+            const PairJob& job = p.job[ji];
+            const TileAt at = tile_at<BN, EPI>(job, t);
             const uint32_t acc = j & 1u;
             const long long row0 = at.m0 + rank * 128 + q * 32;
             const uint32_t taddr = tmem_base + acc * 256u + (static_cast<uint32_t>(q * 32) << 16);
@@ -305,10 +338,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
             for (int c = 0; c < kChunks; c++) {
                 const int cc = half * (kChunks * 64) + c * 64;      // column within the tile's outputs
                 const long long col0 = at.n0 + cc;
-                const int cols = static_cast<int>(max(0ll, min(64ll, p.N - col0)));
+                const int cols = static_cast<int>(max(0ll, min(64ll, job.N - col0)));
                 uint4 res[EPI == EPI_LINEAR ? 8 : 1];
                 if constexpr (EPI == EPI_LINEAR) {
-                    if (p.res.p) load_rows64<T>(p.res, p.res_vec, stg, lane, row0, col0, p.M, cols, res);
+                    if (p.res.p) load_rows64<T>(p.res, p.res_vec, stg, lane, row0, col0, job.M, cols, res);
                 }
                 if (c == 0) {
                     ok = mbar_wait_warp(&tfull_bar[acc], (j >> 1) & 1u, abort_flag, status, 0x400 | (blockIdx.x << 12));
@@ -328,16 +361,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(mapa(smem_u32(&tempty_bar[acc]), 0));
                 }
-                if (cols == 0 || row0 >= p.M) continue;   // (the same for the whole warp)
+                if (cols == 0 || row0 >= job.M) continue;   // (the same for the whole warp)
                 auto put = [&](int which, const float* val) {
-                    store_rows64<T>(p.o[which], &p.out[which], p.out_tma[which], stg, lane, row0, col0, p.M, cols, val);
+                    store_rows64<T>(job.o[which], &job.out[which], job.out_tma[which], stg, lane, row0, col0, job.M, cols, val);
                 };
                 if constexpr (EPI == EPI_PLAIN) {
                     put(at.group, v);
                 } else if constexpr (EPI == EPI_LINEAR) {
                     if (p.bias[0]) add_bias64(p.bias[0], col0, cols, v);
                     if (p.res.p) add_row64<T>(res, v);
-                    if (p.o[1].p) put(1, v);
+                    if (job.o[1].p) put(1, v);
                     with_act(p.act, [&](auto act) {
 #pragma unroll
                         for (int i = 0; i < 64; i += 2) {
@@ -349,8 +382,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
                 } else {
                     if (p.bias[0]) add_bias64(p.bias[0], col0, cols, v);
                     if (p.bias[1]) add_bias64(p.bias[1], col0, cols, u);
-                    if (p.o[1].p) put(1, v);
-                    if (p.o[2].p) put(2, u);
+                    if (job.o[1].p) put(1, v);
+                    if (job.o[2].p) put(2, u);
                     with_act(p.act, [&](auto act) {
 #pragma unroll
                         for (int i = 0; i < 64; i += 2) {
@@ -377,52 +410,106 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
     }
 }
 
-typedef void (*PairFn)(const PairParams);
+int fill_job(const DenseGemm& g, int bn, PairJob* p) {
+    int rc = DLF_OK;
+    for (int i = 0; i < 2 && rc == DLF_OK; i++) {
+        const Mat &a = g.a[i], &b = g.b[i];
+        if (a.p) rc = g.a_mn ? dense_map(&p->a[i], a, g.K, g.M, 64, 64) : dense_map(&p->a[i], a, g.M, g.K, 128, 64);
+        if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p->b[i], b, g.K, g.N, 64, 64) : dense_map(&p->b[i], b, g.N, g.K, bn / 2, 64);
+    }
+    for (int i = 0; i < 3 && rc == DLF_OK; i++) {
+        p->o[i] = g.out[i];
+        p->out_tma[i] = g.out[i].p && dense_rows16(g.out[i]);
+        if (p->out_tma[i]) rc = dense_map(&p->out[i], g.out[i], g.M, g.N, 32, 64);
+    }
+    const int step = g.gated ? bn / 2 : bn;
+    p->M = g.M; p->N = g.N;
+    p->tiles_m = static_cast<int>((g.M + 255) / 256);
+    p->tiles_n = static_cast<int>((g.N + step - 1) / step);
+    p->group_tiles = static_cast<long long>(p->tiles_m) * p->tiles_n;
+    p->tiles = p->group_tiles * g.groups;
+    p->chunks1 = static_cast<int>((g.K + 63) / 64);
+    p->chunks = p->chunks1 * g.sources;
+    p->groups = g.groups;
+    p->amn = g.a_mn;
+    return rc;
+}
+template <typename FN, typename PARAMS>
+int launch_pairs(FN fn, const PARAMS& p, cudaStream_t s) {
+    const int rc = dense_smem_attr(reinterpret_cast<const void*>(fn), kDynSmem);
+    if (rc) return rc;
+    const cudaError_t e = launch_kernel(fn, 2 * p.pairs, kThreads, kDynSmem, s, p);
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
 template <typename T>
-PairFn pick_pair(const DenseGemm& g, int bn) {
-    if (g.gated) return dense_pair_kernel<T, false, false, EPI_GATED, 256>;
-    if (g.a_mn) return bn == 256 ? dense_pair_kernel<T, true, true, EPI_PLAIN, 256> : dense_pair_kernel<T, true, true, EPI_PLAIN, 128>;
-    if (g.b_mn) return bn == 256 ? dense_pair_kernel<T, false, true, EPI_PLAIN, 256> : dense_pair_kernel<T, false, true, EPI_PLAIN, 128>;
-    return bn == 256 ? dense_pair_kernel<T, false, false, EPI_LINEAR, 256> : dense_pair_kernel<T, false, false, EPI_LINEAR, 128>;
+int launch_forward(const DenseGemm& g, int bn, const PairParams<1>& p, cudaStream_t s) {
+    if (g.gated) return launch_pairs(dense_pair_kernel<T, EPI_GATED, 256>, p, s);
+    return bn == 256 ? launch_pairs(dense_pair_kernel<T, EPI_LINEAR, 256>, p, s) : launch_pairs(dense_pair_kernel<T, EPI_LINEAR, 128>, p, s);
+}
+template <typename T>
+int launch_grads(int bn, const PairParams<2>& p, cudaStream_t s) {
+    return bn == 256 ? launch_pairs(dense_pair_kernel<T, EPI_PLAIN, 256>, p, s) : launch_pairs(dense_pair_kernel<T, EPI_PLAIN, 128>, p, s);
 }
 
 }  // namespace
 
-int launch_dense_pair(const DenseGemm& g, int bn, cudaStream_t s) {
+// How the pairs share two jobs' tiles (see PairParams): the least time, in chunks of K, by which every tile has a pair.  Tiles of the second
+// job go to the pairs with one tile less of the first until they are as late as the others.
+double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest, int* few, int* many) {
+    // (a tile's rows take as long as 8 chunks, 2.4 of them before its accumulator is free again)
+    auto tiles = [&](const DenseGemm& q) { return ((q.M + 255) / 256) * ((q.N + (q.gated ? bn / 2 : bn) - 1) / (q.gated ? bn / 2 : bn)) * q.groups; };
+    auto cost = [&](const DenseGemm& q) { return static_cast<double>((q.K + 63) / 64 * q.sources) + 2.4; };
+    const int64_t t0 = tiles(g[0]), t1 = n > 1 ? tiles(g[1]) : 0;
+    const int64_t q0 = t0 / pairs, r = t0 % pairs;
+    *rest = static_cast<int>(r);
+    *few = *many = 0;
+    const double c0 = cost(g[0]);
+    double end = c0 * static_cast<double>(q0 + (r ? 1 : 0));
+    if (t1 == 0) return end;
+    const double c1 = cost(g[1]);
+    // the earliest end at which the places suffice, from the perfectly even one on
+    double T = (c0 * static_cast<double>(t0) + c1 * static_cast<double>(t1)) / pairs;
+    for (int i = 0; i < 1000000; i++) {
+        const int64_t few_n = std::max<int64_t>(0, static_cast<int64_t>((T - c0 * static_cast<double>(q0)) / c1 + 1e-9));
+        const int64_t many_n = std::max<int64_t>(0, static_cast<int64_t>((T - c0 * static_cast<double>(q0 + 1)) / c1 + 1e-9));
+        if (few_n * (pairs - r) + many_n * r >= t1) {
+            *few = static_cast<int>(few_n);
+            *many = static_cast<int>(many_n);
+            return std::max(end, T);
+        }
+        T += c1 / 8;
+    }
+    return -1.0;
+}
+
+int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s) {
     int sms = 0;
     int rc = query_sms(&sms);
     if (rc) return rc;
-    PairParams p;
+    const bool bf = g[0].dtype == DLF_BF16;
+    if (!g[0].b_mn) {
+        PairParams<1> p;
+        std::memset(&p, 0, sizeof(p));
+        rc = fill_job(g[0], bn, &p.job[0]);
+        if (rc) return rc;
+        p.res = g[0].res;
+        p.res_vec = dense_rows16(g[0].res);
+        p.bias[0] = g[0].bias[0]; p.bias[1] = g[0].bias[1];
+        p.act = g[0].act;
+        p.pairs = static_cast<int>(std::min<long long>(p.job[0].tiles, std::max(1, sms / 2)));
+        return bf ? launch_forward<__nv_bfloat16>(g[0], bn, p, s) : launch_forward<__half>(g[0], bn, p, s);
+    }
+    PairParams<2> p;
     std::memset(&p, 0, sizeof(p));
-    for (int i = 0; i < 2 && rc == DLF_OK; i++) {
-        const Mat &a = g.a[i], &b = g.b[i];
-        if (a.p) rc = g.a_mn ? dense_map(&p.a[i], a, g.K, g.M, 64, 64) : dense_map(&p.a[i], a, g.M, g.K, 128, 64);
-        if (b.p && rc == DLF_OK) rc = g.b_mn ? dense_map(&p.b[i], b, g.K, g.N, 64, 64) : dense_map(&p.b[i], b, g.N, g.K, bn / 2, 64);
+    long long tiles = 0;
+    for (int i = 0; i < n; i++) {
+        rc = fill_job(g[i], bn, &p.job[i]);
+        if (rc) return rc;
+        tiles += p.job[i].tiles;
     }
-    for (int i = 0; i < 3 && rc == DLF_OK; i++) {
-        p.o[i] = g.out[i];
-        p.out_tma[i] = g.out[i].p && dense_rows16(g.out[i]);
-        if (p.out_tma[i]) rc = dense_map(&p.out[i], g.out[i], g.M, g.N, 32, 64);
-    }
-    if (rc) return rc;
-    p.res = g.res;
-    p.res_vec = dense_rows16(g.res);
-    p.bias[0] = g.bias[0]; p.bias[1] = g.bias[1];
-    p.M = g.M; p.N = g.N;
-    const int step = g.gated ? bn / 2 : bn;
-    p.tiles_m = static_cast<int>((g.M + 255) / 256);
-    p.tiles_n = static_cast<int>((g.N + step - 1) / step);
-    p.group_tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
-    p.tiles = p.group_tiles * g.groups;
-    p.chunks1 = static_cast<int>((g.K + 63) / 64);
-    p.chunks = p.chunks1 * g.sources;
-    p.act = g.act; p.sources = g.sources; p.groups = g.groups;
-    const int grid = 2 * static_cast<int>(std::min<long long>(p.tiles, sms / 2));
-    const PairFn fn = g.dtype == DLF_BF16 ? pick_pair<__nv_bfloat16>(g, bn) : pick_pair<__half>(g, bn);
-    rc = dense_smem_attr(reinterpret_cast<const void*>(fn), kDynSmem);
-    if (rc) return rc;
-    const cudaError_t e = launch_kernel(fn, grid, kThreads, kDynSmem, s, p);
-    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+    p.pairs = static_cast<int>(std::min<long long>(tiles, std::max(1, sms / 2)));
+    if (dense_pair_share(g, n, bn, p.pairs, &p.rest, &p.few, &p.many) < 0) return DLF_E_UNSUPPORTED;
+    return bf ? launch_grads<__nv_bfloat16>(bn, p, s) : launch_grads<__half>(bn, p, s);
 }
 
 int dense_pair_status(cudaStream_t s, int* code) { return dense_status_of(s, code); }
