@@ -304,7 +304,7 @@ double gemm_bytes(const DenseGemm& g) {
     return 2.0 * (m * k * std::max(g.sources, g.groups) + n * k * (g.gated ? 2 : g.sources) + m * n * g.groups);
 }
 // The longer of two times that overlap, a little more where they are near one another.
-double longer(double a, double b) { return std::pow(std::pow(a, 4.0) + std::pow(b, 4.0), 0.25); }
+double longer(double a, double b) { return std::sqrt(std::sqrt(a * a * a * a + b * b * b * b)); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // 1 if rows start off the 128-byte lines: a tile's row of 128 bytes then takes two of them (777 x 1000 x 1001: 8.9 us with x's rows 1024

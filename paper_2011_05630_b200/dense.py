@@ -48,6 +48,8 @@ def _mat(t, name, shape, like):
         raise ValueError("%s: %s on %s is required, got %s on %s" % (name, like.dtype, like.device, t.dtype, t.device))
     if t.shape != shape:
         raise ValueError("%s: shape %s is required, got %s" % (name, shape, tuple(t.shape)))
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
     ld, step = t.stride()
     if (step != 1 and shape[1] > 1) or (ld < shape[1] and shape[0] > 1):
         raise ValueError("%s: the values of a row have to lie side by side and rows must not overlap (strides %s)" % (name, t.stride()))
@@ -57,7 +59,7 @@ def _mat(t, name, shape, like):
 def _vec(t, name, n, like):
     if t is None:
         return 0
-    if t.dtype is not torch.float32 or t.get_device() != like.get_device() or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not torch.float32 or t.get_device() != like.get_device() or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError("%s: %d float32 values side by side on %s are required" % (name, n, like.device))
     return t.data_ptr()
 
@@ -97,9 +99,9 @@ def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
     xp, ldx = _mat(x, "x", (m, k), x)
     wp, ldw = _mat(w, "w", (n, k), x)
     rp, ldr = _mat(residual, "residual", (m, n), x)
-    y = x.new_empty((m, n)) if out is None else out
+    y = x.new_empty(m, n) if out is None else out
     yp, ldy = (y.data_ptr(), n) if out is None else _mat(y, "out", (m, n), x)
-    z = x.new_empty((m, n)) if save else None
+    z = x.new_empty(m, n) if save else None
     _call("dlf_linear", _LINEAR.pack(dtype, a, m, k, n, xp, wp, _vec(bias, "bias", n, x), rp, yp, z.data_ptr() if save else 0,
                                      ldx, ldw, ldr, ldy, n), x, False)
     return (y, z) if save else y
@@ -119,9 +121,9 @@ def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, nee
     xp, ldx = _mat(x, "x", (m, k), dy)
     wp, ldw = _mat(w, "w", (n, k), dy)
     zp, ldz = _mat(z, "z", (m, n), dy) if a else (0, 0)
-    dx = (torch.empty_like(x) if x is not None else dy.new_empty((m, k))) if need_dx else None
-    dw = (torch.empty_like(w) if w is not None else dy.new_empty((n, k))) if need_dw else None
-    db = dy.new_empty((n,), dtype=torch.float32) if bias else None
+    dx = (torch.empty_like(x) if x is not None else dy.new_empty(m, k)) if need_dx else None
+    dw = (torch.empty_like(w) if w is not None else dy.new_empty(n, k)) if need_dw else None
+    db = dy.new_empty(n, dtype=torch.float32) if bias else None
     dr = torch.empty_like(dy) if residual and a else None
     ptr = lambda t: 0 if t is None else t.data_ptr()
     _call("dlf_linear_grad", _LINEAR_GRAD.pack(dtype, a, m, k, n, dyp, xp, wp, zp, ptr(dx), ptr(dw), ptr(db), ptr(dr),
@@ -137,10 +139,10 @@ def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
     xp, ldx = _mat(x, "x", (m, k), x)
     gp, ldwg = _mat(wg, "wg", (n, k), x)
     up, ldwu = _mat(wu, "wu", (n, k), x)
-    h = x.new_empty((m, n)) if out is None else out
+    h = x.new_empty(m, n) if out is None else out
     hp, ldh = (h.data_ptr(), n) if out is None else _mat(h, "out", (m, n), x)
-    g = x.new_empty((m, n)) if save else None
-    u = x.new_empty((m, n)) if save else None
+    g = x.new_empty(m, n) if save else None
+    u = x.new_empty(m, n) if save else None
     _call("dlf_gated", _GATED.pack(dtype, a, m, k, n, xp, gp, up, _vec(bg, "bg", n, x), _vec(bu, "bu", n, x), hp,
                                    g.data_ptr() if save else 0, u.data_ptr() if save else 0, ldx, ldwg, ldwu, ldh, n, n), x, False)
     return (h, g, u) if save else h
@@ -160,9 +162,9 @@ def gated_backward(dh, x, wg, wu, g, u, act="silu", bias=False, need_dx=True, ne
     wup, ldwu = _mat(wu, "wu", (n, k), dh)
     gp, ldg = _mat(g, "g", (m, n), dh)
     up, ldu = _mat(u, "u", (m, n), dh)
-    dx = (torch.empty_like(x) if x is not None else dh.new_empty((m, k))) if need_dx else None
-    dwg, dwu = (torch.empty_like(wg) if wg is not None else dh.new_empty((n, k)) for _ in range(2)) if need_dw else (None, None)
-    dbg, dbu = (dh.new_empty((n,), dtype=torch.float32) for _ in range(2)) if bias else (None, None)
+    dx = (torch.empty_like(x) if x is not None else dh.new_empty(m, k)) if need_dx else None
+    dwg, dwu = (torch.empty_like(wg) if wg is not None else dh.new_empty(n, k) for _ in range(2)) if need_dw else (None, None)
+    dbg, dbu = (dh.new_empty(n, dtype=torch.float32) for _ in range(2)) if bias else (None, None)
     ptr = lambda t: 0 if t is None else t.data_ptr()
     _call("dlf_gated_grad", _GATED_GRAD.pack(dtype, a, m, k, n, dhp, xp, wgp, wup, gp, up, ptr(dx), ptr(dwg), ptr(dwu), ptr(dbg),
                                              ptr(dbu), lddh, ldx, ldwg, ldwu, ldg, ldu, k, k, k), dh, True)
