@@ -314,7 +314,7 @@ double off_lines(const Mat (&m)[2]) { return (m[0].ld | (m[1].p ? m[1].ld : 0)) 
 double lat_cost(const DenseGemm* g, int n, int sms, DenseLatChoice* best) {
     double least = -1.0;
     DenseLatChoice c{};
-    for (c.bn = 64; c.bn <= 128; c.bn += 64)
+    for (c.bn = 64; c.bn <= 128; c.bn += g[0].b_mn ? 64 : 32)   // (an operand across K comes in boxes of 64)
         for (c.split = 1; c.split <= 8; c.split *= 2) {
             int64_t ctas[2] = {}, all = 0;
             for (int j = 0; j < n; j++) all += ctas[j] = ceil_div(g[j].M, 128) * ceil_div(g[j].N, g[j].gated ? c.bn / 2 : c.bn) * g[j].groups * c.split;

@@ -50,7 +50,7 @@ inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 
 int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s);
 double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest, int* few, int* many);   // chunks of K until the last pair is done
 int dense_pair_status(cudaStream_t s, int* code);             // waits for the stream; a kernel's bounded wait that gave up
-// dense_lat.cu: tiles of at most 128 rows by `bn` columns of B (64 or 128; both halves of a gated tile), K shared out over `split` CTAs (1, 2,
+// dense_lat.cu: tiles of at most 128 rows by `bn` columns of B (64, 128, forward 96, too; both halves of a gated tile), K shared out over `split` CTAs (1, 2,
 // 4, 8).
 struct DenseLatChoice {
     int bn, split;

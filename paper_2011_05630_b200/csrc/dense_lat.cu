@@ -223,7 +223,8 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         const int q = warp & 3, half = warp >> 2, m = q * 32 + lane;
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
         const int out_bn = EPI == EPI_GATED ? P.BN / 2 : P.BN;
-        const int my_rows = max(0, min(p.rows_per, live - rank * p.rows_per)), lg = __ffs(out_bn) - 4;   // (runs of 8 in a row: a power of two)
+        const int my_rows = max(0, min(p.rows_per, live - rank * p.rows_per)), runs = p.vec ? out_bn / 8 : out_bn / 8 + 1;   // (of 8 outputs in a row: below)
+        const uint32_t by_runs = 65536u / static_cast<uint32_t>(runs) + 1u;                                 // i / runs for the at most 2176 runs of a tile
         const long long row_first = m0 + rank * p.rows_per;
         const int n_cols = static_cast<int>(min(static_cast<long long>(out_bn), p.N - n0));
         if (EPI != EPI_PLAIN && threadIdx.x < P.BN) {
@@ -233,18 +234,15 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
         }
         // A run is 8 outputs that are a piece of 16 bytes in memory: where rows start off the 16-byte boundaries, a row's first and
         // last runs are not whole.  Run i of this CTA: row and first column (of n_cols), negative behind the last run.
-        const int runs = p.vec ? 1 << lg : (1 << lg) + 1, total = my_rows * runs;
+        const int total = my_rows * runs;
         const unsigned short* const out0 = static_cast<const unsigned short*>(p.o[EPI == EPI_PLAIN ? group : 0].p) + row_first * p.o[EPI == EPI_PLAIN ? group : 0].ld + n0;
         const int64_t out_ld = p.o[EPI == EPI_PLAIN ? group : 0].ld;
         auto run_at = [&](auto vec, int i, int* c) {
             if (i >= total) return -1;
-            if (vec.value) {
-                const int r = i >> lg;
-                *c = (i - (r << lg)) * 8;
-                return *c < n_cols ? r : -1;
-            }
-            const int r = i / runs;
-            *c = (i - r * runs) * 8 - static_cast<int>((reinterpret_cast<uintptr_t>(out0 + r * out_ld) >> 1) & 7);
+            const int r = static_cast<int>(static_cast<uint32_t>(i) * by_runs >> 16);
+            *c = (i - r * runs) * 8;
+            if (vec.value) return *c < n_cols ? r : -1;
+            *c -= static_cast<int>((reinterpret_cast<uintptr_t>(out0 + r * out_ld) >> 1) & 7);
             return *c < n_cols && *c + 8 > 0 ? r : -1;
         };
         // 8 values of a row from column c on, those that exist
