@@ -380,6 +380,55 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
 
 
+def test_two_threads_at_once():
+    """Two host threads, a stream each, the same calls over and over: each has its own results."""
+    import threading
+    k, n = 320, 712
+    sets, want = [], []
+    for m in (3, 90):
+        mk = Maker(m, torch.float16)
+        sets.append([mk.mat(m, k), mk.mat(m, k), mk.mat(n, k, k ** -0.5), mk.mat(n, k, k ** -0.5), mk.mat(k, n, n ** -0.5), mk.mat(m, k)])
+        want.append(block(*sets[-1]))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(30):
+                    got = block(*sets[i])
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(p, q) for p, q in zip(got, want[i])):
+                    wrong.append(i)
+        except Exception as e:
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+
+
+def test_wrong_tensors_are_refused():
+    mk = Maker(1, torch.float16)
+    x, w, y = mk.mat(4, 64), mk.mat(40, 64), mk.mat(4, 40)
+    for f in (lambda: dense.linear(x, w.bfloat16()), lambda: dense.linear(x.float(), w), lambda: dense.linear(x, mk.mat(40, 56)), lambda: dense.linear(x[0], w),
+              lambda: dense.linear(x, mk.mat(64, 40).t()), lambda: dense.linear(x[:1].expand(4, 64), w), lambda: dense.linear(x, w, act="tanh"),
+              lambda: dense.linear(x, w, bias=y[0]), lambda: dense.linear(x, w, bias=mk.vec(80)[::2]), lambda: dense.linear(x, w, residual=mk.mat(4, 41)),
+              lambda: dense.linear(x, w, out=mk.mat(5, 40)), lambda: dense.linear(x, w.cpu()), lambda: dense.linear_backward(y, x, w, act="gelu"),
+              lambda: dense.linear_backward(y, None, w), lambda: dense.linear_backward(y, x, None), lambda: dense.gated(x, w, mk.mat(41, 64)),
+              lambda: dense.gated_backward(y, x, w, w, y, None), lambda: dense.gated_backward(y, x, None, w, y, y)):
+        with pytest.raises(ValueError):
+            f()
+    from paper_2011_05630_b200 import binding as B
+    for f in (lambda: dense.linear(x, mk.mat(0, 64)), lambda: dense.linear(mk.mat(4, 0), mk.mat(40, 0)), lambda: dense.linear(x, mk.mat(64, 64), out=x)):
+        with pytest.raises(B.DlfError):
+            f()
+    dense.synchronize()
+
+
 def test_offsets_beyond_32_bits():
     """Two thousand million values in an output and in the residual; the last rows are where an offset of 32 bits goes wrong."""
     m, k, n = 270000, 64, 8192
