@@ -86,16 +86,18 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
         Run<T, V> d, e;
 #pragma unroll
         for (int i = 0; i < VP; i++) {
+            constexpr bool kCorner = ACT == DLF_ACT_RELU || ACT == DLF_ACT_RELU6;   // (its slope chooses, last)
             float2 value, slope;
-            const float2 t = dy.get2(i);
+            float2 t = dy.get2(i);
             act_grad2<ACT>(kWithZ ? z.get2(i) : t, &value, &slope);
             if (GATED) {
                 const float2 q = mul2(t, value);
                 s1[i] = add2(s1[i], q);
                 e.set2(i, q);
-                slope = mul2(slope, u.get2(i));
+                if (kCorner) t = mul2(t, u.get2(i));
+                else slope = mul2(slope, u.get2(i));
             }
-            const float2 q = mul2(t, slope);
+            const float2 q = behind2<ACT>(t, slope);
             s0[i] = add2(s0[i], q);
             d.set2(i, q);
         }

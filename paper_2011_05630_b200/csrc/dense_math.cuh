@@ -144,6 +144,13 @@ __device__ __forceinline__ void act_grad2(float2 v, float2* value, float2* slope
         *slope = fma2(*value, dt, s);
     }
 }
+// A gradient behind act: d slope.  At a corner or beyond, ReLU and ReLU6 are constant and nothing comes through: 0 whatever d is, infinities
+// and NaN too (as in automatic differentiation; a product would make a NaN of them, and that a row of dx and of dw).
+template <int ACT>
+__device__ __forceinline__ float2 behind2(float2 d, float2 slope) {
+    if (ACT == DLF_ACT_RELU || ACT == DLF_ACT_RELU6) return make_float2(slope.x != 0.0f ? d.x : 0.0f, slope.y != 0.0f ? d.y : 0.0f);
+    return mul2(d, slope);
+}
 template <int ACT>
 __device__ __forceinline__ float act_f(float v) { return act2<ACT>(make_float2(v, v)).x; }
 
