@@ -303,6 +303,8 @@ int dlf_conv_chain_run_static(const dlf_layer_desc* layers, int n_layers, int N,
  * Their derivatives are taken at z and g as the forward call stored them; at a corner of RELU and RELU6 the derivative is 0.
  * Where RELU and RELU6 are closed (at and beyond a corner, and at a NaN) dz and dg are 0 even if dy, dh or u is infinite or NaN; else infinities
  * and NaN follow from the formulas.
+ * GELU, GELU_TANH and SILU are good to 2^-15 of their own value before they are rounded, however small it is (GELU down to v = -12.5, GELU_TANH to
+ * -9, SILU to -80; 0 at last beyond), their derivatives to 2^-15 of the absolute terms.
  * dz, dg and du are rounded to 16 bits, once, before they enter the products (db, dbg and dbu sum the values before that).
  *
  * Optional (null): bias, res, z, bg, bu, g, u of the forward calls; every output of the backward calls, and the inputs that

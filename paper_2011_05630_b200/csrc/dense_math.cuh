@@ -85,16 +85,21 @@ __device__ __forceinline__ float2 sigmoid2(float2 v) { return rcp2(add2(exp2_2(m
 constexpr float kGeluC = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGeluA = 0.044715f;
 
-// The normal distribution's density at v and its integral up to v: erfc by the rational approximation 7.1.26 of Abramowitz and Stegun,
-// "Handbook of Mathematical Functions" (off by at most 1.5e-7, half of that here), which shares its exponential with the density.
+// The normal distribution's density at v and its integral up to v.  The integral up to -a is e^(-a^2 / 2) t Q(t) with t = 1 / (1 + 0.306 a), Q
+// the polynomial of degree 7 with the least largest relative error over a from 0 to 15, 1.1e-7 (fitted by reweighted least squares): it
+// shares its exponential with the density, and is as exact in the tail, where it is small, as in the middle (with the exponential's
+// argument rounded, 6e-7 of the value down to -3, 2e-6 to -6, 8e-6 to -13).
 __device__ __forceinline__ void normal2(float2 v, float2* density, float2* integral) {
     const float2 a = make_float2(fabsf(v.x), fabsf(v.y));
     const float2 e = exp2_2(mul2(mul2(v, v), both(-0.5f * kLog2e)));
-    const float2 t = rcp2(fma2(a, both(0.3275911f * 0.7071067811865476f), both(1.0f)));
-    float2 s = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
-    s = fma2(t, s, both(0.5f * 1.421413741f));
-    s = fma2(t, s, both(0.5f * -0.284496736f));
-    s = fma2(t, s, both(0.5f * 0.254829592f));
+    const float2 t = rcp2(fma2(a, both(0.306f), both(1.0f)));
+    float2 s = fma2(t, both(0.03653757f), both(-0.15069884f));
+    s = fma2(t, s, both(0.17938326f));
+    s = fma2(t, s, both(-0.033034489f));
+    s = fma2(t, s, both(0.11862855f));
+    s = fma2(t, s, both(0.104367666f));
+    s = fma2(t, s, both(0.12277222f));
+    s = fma2(t, s, both(0.1220441f));
     const float2 tail = mul2(mul2(t, e), s), rest = fma2(tail, both(-1.0f), both(1.0f));
     *integral = make_float2(v.x < 0.0f ? tail.x : rest.x, v.y < 0.0f ? tail.y : rest.y);
     *density = mul2(e, both(0.3989422804014327f));
