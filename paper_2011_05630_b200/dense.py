@@ -8,7 +8,8 @@
 Matrices are two-dimensional CUDA tensors of one 16-bit type (float16 or bfloat16) on one device; rows may lie any distance apart
 (`x[:, :k]` of a wider tensor is fine), the values of a row side by side.  Weights are [out][in], biases float32.  Every call
 enqueues on the current stream of the tensors' device and computes inside libdlfusion.so (see include/dlfusion.h for the formulas
-and their roundings); PyTorch allocates the outputs and, where a call needs one, its workspace.  Nothing is recorded for autograd.
+and their roundings); PyTorch allocates the outputs and, where a call needs one, its workspace.  Nothing is recorded for autograd: while autograd
+records (outside torch.no_grad() and a Function's forward and backward), tensors that require gradients are refused.
 """
 from __future__ import annotations
 
@@ -27,7 +28,8 @@ _GATED_GRAD = struct.Struct("@ii3q11P9q")
 _ops = {}   # name -> (call, its workspace query)
 
 
-def _enter(x, act):
+def _enter(x, act, *others):
+    """What a call's first matrix and its activation are to the library, once nothing speaks against the call as such."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("a CUDA tensor is required: there is no CPU path")
     dtype, a = _DTYPES.get(x.dtype), B.DENSE_ACTS.get(act)
@@ -37,6 +39,10 @@ def _enter(x, act):
         raise ValueError("act is one of %s, got %r" % (", ".join(B.DENSE_ACTS), act))
     if x.dim() != 2:
         raise ValueError("matrices have two dimensions, got %d" % x.dim())
+    if torch.is_grad_enabled():
+        for t in (x, *others):
+            if t is not None and t.requires_grad:
+                raise ValueError("a tensor requires a gradient, and nothing would be recorded for it: call under torch.no_grad(), or with detached tensors")
     return dtype, a
 
 
@@ -93,7 +99,7 @@ def synchronize(device=None):
 def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
     """y = act(x w^T + bias + residual) for x [m][k], w [n][k], residual [m][n]; with `save` (y, z), z being the sum that the
     activation was applied to.  `out` receives y and may be the residual itself."""
-    dtype, a = _enter(x, act)
+    dtype, a = _enter(x, act, w, bias, residual, out)
     m, k = x.shape
     n = w.shape[0]
     xp, ldx = _mat(x, "x", (m, k), x)
@@ -110,7 +116,7 @@ def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
 def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, need_dx=True, need_dw=True):
     """(dx, dw, db, dr): the gradients of `linear`'s inputs, None for one that is not asked for.  z: what `linear(..., save=True)`
     kept, needed with an activation.  dr, the residual's gradient, is dy itself where there is no activation."""
-    dtype, a = _enter(dy, act)
+    dtype, a = _enter(dy, act, x, w, z)
     m, n = dy.shape
     k = x.shape[1] if x is not None else w.shape[1] if w is not None else 1
     if a and z is None:
@@ -133,7 +139,7 @@ def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, nee
 
 def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
     """h = act(x wg^T + bg) * (x wu^T + bu) for x [m][k], wg and wu [n][k]; with `save` (h, g, u), g and u being the two sums."""
-    dtype, a = _enter(x, act)
+    dtype, a = _enter(x, act, wg, wu, bg, bu, out)
     m, k = x.shape
     n = wg.shape[0]
     xp, ldx = _mat(x, "x", (m, k), x)
@@ -151,7 +157,7 @@ def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
 def gated_backward(dh, x, wg, wu, g, u, act="silu", bias=False, need_dx=True, need_dw=True):
     """(dx, dwg, dwu, dbg, dbu): the gradients of `gated`'s inputs, None for one that is not asked for.  g and u: what
     `gated(..., save=True)` kept."""
-    dtype, a = _enter(dh, act)
+    dtype, a = _enter(dh, act, x, wg, wu, g, u)
     m, n = dh.shape
     k = x.shape[1] if x is not None else wg.shape[1] if wg is not None else 1
     if (need_dw and x is None) or (need_dx and (wg is None or wu is None)) or g is None or u is None:
