@@ -7,6 +7,7 @@
 #include <cxxabi.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -44,7 +45,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 int encode_tmap(void* out_map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                 const uint32_t* box, const uint32_t* elem_strides) {
-    static EncodeTiledFn fn = nullptr;
+    static std::atomic<EncodeTiledFn> found{nullptr};
+    EncodeTiledFn fn = found.load(std::memory_order_acquire);
     if (!fn) {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult qr;
@@ -52,6 +54,7 @@ int encode_tmap(void* out_map, const void* base, int rank, const uint64_t* dims,
         if (e != cudaSuccess) return cuda_fail(e);
         if (qr != cudaDriverEntryPointSuccess || !p) return cuda_fail_drv(999);
         fn = reinterpret_cast<EncodeTiledFn>(p);
+        found.store(fn, std::memory_order_release);
     }
     cuuint64_t gd[5], gs[4];
     cuuint32_t bx[5], es[5];
@@ -61,9 +64,21 @@ int encode_tmap(void* out_map, const void* base, int rank, const uint64_t* dims,
         es[i] = elem_strides[i];
         if (i < rank - 1) gs[i] = strides_bytes[i];
     }
-    CUresult r = fn(static_cast<CUtensorMap*>(out_map), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, static_cast<cuuint32_t>(rank),
-                    const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    auto encode = [&] {
+        return fn(static_cast<CUtensorMap*>(out_map), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, static_cast<cuuint32_t>(rank),
+                  const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r == CUDA_ERROR_INVALID_CONTEXT) {
+        // A host thread has its device's context once it has made a call of the runtime that needs one; of the driver's calls this one needs it,
+        // too, and may be a thread's first (in a training loop's backward pass, say).
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess) e = cudaSetDevice(dev);
+        if (e != cudaSuccess) return cuda_fail(e);
+        r = encode();
+    }
     if (r != CUDA_SUCCESS) return cuda_fail_drv(static_cast<int>(r));
     return DLF_OK;
 }
