@@ -369,9 +369,13 @@ int dlf_gated(const dlf_gated_args* args, void* workspace_dev, size_t bytes, voi
 int dlf_gated_grad_workspace_bytes(const dlf_gated_grad_args* args, size_t* bytes);
 int dlf_gated_grad(const dlf_gated_grad_args* args, void* workspace_dev, size_t bytes, void* stream);
 /* Waits for the stream and reports what went wrong with the dense operators' kernels: DLF_E_CUDA for a CUDA error, DLF_E_TIMEOUT if
- * a bounded device-side wait gave up in any of them on the current device since the last such report (their outputs are then undefined).
+ * a bounded device-side wait gave up in any of them on the current device, whatever the stream, since the calling thread's last such report (their outputs
+ * are then undefined).  Every thread is told, and only here: other calls, a plain synchronisation among them, say nothing of it.
  * Not for streams that are being captured. */
 int dlf_dense_sync(void* stream);
+/* Self-test of that report, as dlf_net_debug_stall is for nets: enqueues a one-CTA kernel whose wait gives up after limit_us (1 to 1000000)
+ * microseconds, in the place of the pairs' kernels (which 0) or the clusters' (1). */
+int dlf_dense_debug_stall(int which, int limit_us, void* stream);
 
 #ifdef __cplusplus
 }

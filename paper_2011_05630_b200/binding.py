@@ -85,6 +85,7 @@ def lib():
                                                     C.POINTER(vp), C.POINTER(vp), vp, C.c_int, vp]),
         }
         sig["dlf_dense_sync"] = (C.c_int, [vp])
+        sig["dlf_dense_debug_stall"] = (C.c_int, [C.c_int, C.c_int, vp])
         for op in ("dlf_linear", "dlf_linear_grad", "dlf_gated", "dlf_gated_grad"):   # (their arguments: a packed struct)
             sig[op] = (C.c_int, [C.c_char_p, vp, C.c_size_t, vp])
             sig[op + "_workspace_bytes"] = (C.c_int, [C.c_char_p, C.POINTER(C.c_size_t)])

@@ -695,14 +695,23 @@ int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
 extern "C" {
 
 int dlf_dense_sync(void* stream) {
-    int code = 0;
-    int rc = dlf::dense_pair_status(static_cast<cudaStream_t>(stream), &code);
-    if (rc == DLF_OK) {
-        int lat = 0;
-        rc = dlf::dense_lat_status(static_cast<cudaStream_t>(stream), &lat);
-        code |= lat;
-    }
-    return rc ? rc : code ? DLF_E_TIMEOUT : DLF_OK;
+    static thread_local int told[dlf::kMaxDevices][2];   // what this thread has been told of
+    const int dev = dlf::current_device_slot();
+    if (dev < 0) return DLF_E_UNSUPPORTED;
+    int now[2] = {0, 0};
+    int rc = dlf::dense_pair_gave_up(static_cast<cudaStream_t>(stream), &now[0]);
+    if (rc == DLF_OK) rc = dlf::dense_lat_gave_up(static_cast<cudaStream_t>(stream), &now[1]);
+    if (rc) return rc;
+    const bool more = now[0] != told[dev][0] || now[1] != told[dev][1];
+    told[dev][0] = now[0];
+    told[dev][1] = now[1];
+    return more ? DLF_E_TIMEOUT : DLF_OK;
+}
+
+int dlf_dense_debug_stall(int which, int limit_us, void* stream) {
+    if ((which != 0 && which != 1) || limit_us < 1 || limit_us > 1000000) return DLF_E_INVALID_ARG;
+    const unsigned long long ns = static_cast<unsigned long long>(limit_us) * 1000;
+    return which ? dlf::dense_lat_stall(ns, static_cast<cudaStream_t>(stream)) : dlf::dense_pair_stall(ns, static_cast<cudaStream_t>(stream));
 }
 
 int dlf_linear_workspace_bytes(const dlf_linear_args* a, size_t* bytes) { return bytes ? dlf::linear(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }

@@ -49,7 +49,8 @@ inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 
 // dense_tc.cu: tiles of 256 rows by bn (256, 128; gated: 256, both halves) columns of B; operands with rows on 16-byte boundaries.
 int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s);
 double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest, int* few, int* many);   // chunks of K until the last pair is done
-int dense_pair_status(cudaStream_t s, int* code);             // waits for the stream; a kernel's bounded wait that gave up
+int dense_pair_gave_up(cudaStream_t s, int* count);           // waits for the stream; CTAs in which a bounded wait has given up so far
+int dense_pair_stall(unsigned long long limit_ns, cudaStream_t s);   // a wait that does
 // dense_lat.cu: tiles of at most 128 rows by `bn` columns of B (64, 128, forward 96, too; both halves of a gated tile), K shared out over `split` CTAs (1, 2,
 // 4, 8).
 struct DenseLatChoice {
@@ -58,7 +59,8 @@ struct DenseLatChoice {
 };
 bool dense_lat_possible(const DenseGemm& g, const DenseLatChoice& c, int* rows, int* stages, bool* two);   // `two` of its CTAs fit an SM
 int launch_dense_lat(const DenseGemm* g, int n, const DenseLatChoice& c, cudaStream_t s);
-int dense_lat_status(cudaStream_t s, int* code);
+int dense_lat_gave_up(cudaStream_t s, int* count);
+int dense_lat_stall(unsigned long long limit_ns, cudaStream_t s);
 
 bool dense_gemv_takes(const DenseGemm& g);                           // dense_gemv.cu: forward products of a few tokens, any rows
 int launch_dense_gemv(const DenseGemm& g, cudaStream_t s);

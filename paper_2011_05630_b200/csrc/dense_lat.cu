@@ -91,7 +91,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
     uint8_t* sbase = smem_raw + (base - smem_u32(smem_raw));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &abort_s;
-    int* status = &g_dense_status;
+    int* status = g_dense_status;
     const int rank = SPLIT > 1 ? static_cast<int>(cluster_rank()) : 0;
     long long tile = (static_cast<int>(blockIdx.x) - (job1 ? P.first1 : 0)) / SPLIT;
     const int group = p.groups > 1 && tile >= p.group_tiles ? 1 : 0;
@@ -373,6 +373,7 @@ __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(kThreads, SPLIT 
     if (SPLIT > 1 && warp >= kEpiWarps) cluster_wait();
     __syncthreads();
     if (warp == kMmaWarp) {
+        if (lane == 0 && (abort_s || red_abort_s)) dense_count_abort();
         if (abort_s) __nanosleep(20000);   // let copies in flight land before the CTA retires
         tc_fence_after_sync();
         tmem_dealloc(tmem_base, kMaxBN * kMmaWarps);
@@ -485,6 +486,7 @@ int launch_dense_lat(const DenseGemm* g, int n, const DenseLatChoice& c, cudaStr
     return bf ? launch_split<__nv_bfloat16, EPI_PLAIN>(c.split, p, grid, smem, s) : launch_split<__half, EPI_PLAIN>(c.split, p, grid, smem, s);
 }
 
-int dense_lat_status(cudaStream_t s, int* code) { return dense_status_of(s, code); }
+int dense_lat_gave_up(cudaStream_t s, int* count) { return dense_gave_up(s, count); }
+int dense_lat_stall(unsigned long long limit_ns, cudaStream_t s) { return dense_stall(limit_ns, s); }
 
 }  // namespace dlf

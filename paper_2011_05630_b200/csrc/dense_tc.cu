@@ -214,7 +214,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = static_cast<int>(cluster_rank());
     volatile int* abort_flag = &abort_s;
-    int* status = &g_dense_status;
+    int* status = g_dense_status;
     const int pair = static_cast<int>(blockIdx.x) >> 1;
     int ji = 0;          // a tile's job and number
     long long t = 0;
@@ -404,7 +404,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) dense_p
     cluster_arrive();
     cluster_wait();
     if (warp == kMmaWarp) {
-        if (abort_s) __nanosleep(20000);
+        if (abort_s) {
+            if (lane == 0) dense_count_abort();
+            __nanosleep(20000);
+        }
         tc_fence_after_sync();
         tmem_dealloc_pair(tmem_base, 512);
     }
@@ -512,6 +515,7 @@ int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s) {
     return bf ? launch_grads<__nv_bfloat16>(bn, p, s) : launch_grads<__half>(bn, p, s);
 }
 
-int dense_pair_status(cudaStream_t s, int* code) { return dense_status_of(s, code); }
+int dense_pair_gave_up(cudaStream_t s, int* count) { return dense_gave_up(s, count); }
+int dense_pair_stall(unsigned long long limit_ns, cudaStream_t s) { return dense_stall(limit_ns, s); }
 
 }  // namespace dlf

@@ -12,8 +12,9 @@
 
 namespace dlf {
 
-// One for each source file that includes this (see dense_status_of).
-static __device__ int g_dense_status;
+// Where a bounded wait first gave up, and the number of CTAs in which one has so far: never cleared, so that no report can take another's.  One for
+// each source file that includes this: what names it is static.
+static __device__ int g_dense_status[2];
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 // A map over a matrix of `rows` rows of `cols` values (any 16-bit type: the copies move bits), boxes of box_rows x box_cols.
@@ -43,21 +44,37 @@ inline int dense_smem_attr(const void* fn, int bytes) {
     return DLF_OK;
 }
 
-// Waits for the stream and reads the status word; a code in it is reported once.
-inline int dense_status_of(cudaStream_t s, int* code) {
-    cudaError_t e = cudaMemcpyFromSymbolAsync(code, g_dense_status, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
+// Waits for the stream and reads the number of CTAs in which a wait has given up.
+static int dense_gave_up(cudaStream_t s, int* count) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(count, g_dense_status, sizeof(int), sizeof(int), cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e != cudaSuccess) return cuda_fail(e);
-    if (*code) {
-        const int zero = 0;
-        e = cudaMemcpyToSymbolAsync(g_dense_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-        if (e != cudaSuccess) return cuda_fail(e);
-    }
-    return DLF_OK;
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
 // ---- device ----------------------------------------------------------------------------------------------------------------
+// At a CTA's end, by one thread.
+static __device__ __forceinline__ void dense_count_abort() { atomicAdd(&g_dense_status[1], 1); }
+
+// A wait at a barrier that nothing arrives at, as the kernels wait (see dlf_dense_debug_stall).
+static __global__ void dense_stall_kernel(unsigned long long limit_ns) {
+    __shared__ uint64_t bar;
+    __shared__ int abort_s;
+    if (threadIdx.x == 0) {
+        abort_s = 0;
+        mbar_init(&bar, 1);
+        fence_barrier_init();
+    }
+    __syncthreads();
+    mbar_wait(&bar, 0u, &abort_s, g_dense_status, 0xf00, limit_ns);
+    __syncthreads();
+    if (abort_s && threadIdx.x == 0) dense_count_abort();
+}
+static int dense_stall(unsigned long long limit_ns, cudaStream_t s) {
+    dense_stall_kernel<<<1, 64, 0, s>>>(limit_ns);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? DLF_OK : cuda_fail(e);
+}
+
 // Instruction descriptor: fp16 or bf16 operands (bits 7 and 10), fp32 sums; bits 15 and 16: operand A, B across K.
 template <typename T>
 __host__ __device__ constexpr uint32_t dense_idesc(int m, int n, bool amn, bool bmn) {
