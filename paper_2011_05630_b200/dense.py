@@ -46,6 +46,13 @@ def _enter(x, act, *others):
     return dtype, a
 
 
+def _size(t, name, i):
+    """Rows (i 0) or columns (1) of what has to be a matrix."""
+    if t.dim() != 2:
+        raise ValueError("%s: matrices have two dimensions, got %d" % (name, t.dim()))
+    return t.shape[i]
+
+
 def _mat(t, name, shape, like):
     """(pointer, row length) of a matrix, or what is wrong with it."""
     if t is None:
@@ -101,7 +108,7 @@ def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
     activation was applied to.  `out` receives y and may be the residual itself."""
     dtype, a = _enter(x, act, w, bias, residual, out)
     m, k = x.shape
-    n = w.shape[0]
+    n = _size(w, "w", 0)
     xp, ldx = _mat(x, "x", (m, k), x)
     wp, ldw = _mat(w, "w", (n, k), x)
     rp, ldr = _mat(residual, "residual", (m, n), x)
@@ -118,7 +125,7 @@ def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, nee
     kept, needed with an activation.  dr, the residual's gradient, is dy itself where there is no activation."""
     dtype, a = _enter(dy, act, x, w, z)
     m, n = dy.shape
-    k = x.shape[1] if x is not None else w.shape[1] if w is not None else 1
+    k = _size(x, "x", 1) if x is not None else _size(w, "w", 1) if w is not None else 1
     if a and z is None:
         raise ValueError("z: the sum that the forward call kept is required with an activation")
     if (need_dw and x is None) or (need_dx and w is None):
@@ -141,7 +148,7 @@ def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
     """h = act(x wg^T + bg) * (x wu^T + bu) for x [m][k], wg and wu [n][k]; with `save` (h, g, u), g and u being the two sums."""
     dtype, a = _enter(x, act, wg, wu, bg, bu, out)
     m, k = x.shape
-    n = wg.shape[0]
+    n = _size(wg, "wg", 0)
     xp, ldx = _mat(x, "x", (m, k), x)
     gp, ldwg = _mat(wg, "wg", (n, k), x)
     up, ldwu = _mat(wu, "wu", (n, k), x)
@@ -159,7 +166,7 @@ def gated_backward(dh, x, wg, wu, g, u, act="silu", bias=False, need_dx=True, ne
     `gated(..., save=True)` kept."""
     dtype, a = _enter(dh, act, x, wg, wu, g, u)
     m, n = dh.shape
-    k = x.shape[1] if x is not None else wg.shape[1] if wg is not None else 1
+    k = _size(x, "x", 1) if x is not None else _size(wg, "wg", 1) if wg is not None else 1
     if (need_dw and x is None) or (need_dx and (wg is None or wu is None)) or g is None or u is None:
         raise ValueError("g and u are required, x for the weights' gradients, wg and wu for dx")
     dhp, lddh = _mat(dh, "dh", (m, n), dh)
