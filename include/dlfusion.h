@@ -368,6 +368,13 @@ int dlf_gated_workspace_bytes(const dlf_gated_args* args, size_t* bytes);
 int dlf_gated(const dlf_gated_args* args, void* workspace_dev, size_t bytes, void* stream);
 int dlf_gated_grad_workspace_bytes(const dlf_gated_grad_args* args, size_t* bytes);
 int dlf_gated_grad(const dlf_gated_grad_args* args, void* workspace_dev, size_t bytes, void* stream);
+/* Which kernels these calls launch with these arguments, in their order, on a GPU of sm_count SMs (0: the current device), without launching any: text,
+ * "kernel(choice=value ...); ...", cut off at `bytes` with its end.  Looks at what dlf_*_workspace_bytes looks at, too, and refuses what the call refuses (but
+ * for the workspace); with an sm_count it makes no call of CUDA's.  The choices are for reading and tests: they change as the estimates do. */
+int dlf_linear_kernels(const dlf_linear_args* args, int sm_count, char* text, size_t bytes);
+int dlf_linear_grad_kernels(const dlf_linear_grad_args* args, int sm_count, char* text, size_t bytes);
+int dlf_gated_kernels(const dlf_gated_args* args, int sm_count, char* text, size_t bytes);
+int dlf_gated_grad_kernels(const dlf_gated_grad_args* args, int sm_count, char* text, size_t bytes);
 /* Waits for the stream and reports what went wrong with the dense operators' kernels: DLF_E_CUDA for a CUDA error, DLF_E_TIMEOUT if
  * a bounded device-side wait gave up in any of them on the current device, whatever the stream, since the calling thread's last such report (their outputs
  * are then undefined).  Every thread is told, and only here: other calls, a plain synchronisation among them, say nothing of it.

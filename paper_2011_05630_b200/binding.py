@@ -89,6 +89,7 @@ def lib():
         for op in ("dlf_linear", "dlf_linear_grad", "dlf_gated", "dlf_gated_grad"):   # (their arguments: a packed struct)
             sig[op] = (C.c_int, [C.c_char_p, vp, C.c_size_t, vp])
             sig[op + "_workspace_bytes"] = (C.c_int, [C.c_char_p, C.POINTER(C.c_size_t)])
+            sig[op + "_kernels"] = (C.c_int, [C.c_char_p, C.c_int, C.c_char_p, C.c_size_t])
         for name, (res, args) in sig.items():
             f = getattr(L, name)
             f.restype, f.argtypes = res, args

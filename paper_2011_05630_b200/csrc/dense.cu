@@ -3,6 +3,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdarg>
+#include <cstdio>
 #include <initializer_list>
 #include <type_traits>
 
@@ -228,6 +230,23 @@ GradFn pick_grad(bool gated, bool wide, int act) {
     return wide ? pick_grad_act<T, V, false, true>(act) : pick_grad_act<T, V, false, false>(act);
 }
 
+// How the pass runs: 8 values at a time or 2 (see Run), wide strips or narrow ones, CTAs.
+struct GradLayout {
+    bool v8, wide;
+    int grid;
+};
+GradLayout grad_layout(const DenseGrad& g, int sms) {
+    auto vec = [](const Mat& m) { return !m.p || (aligned(16, m.p) && m.ld % 8 == 0); };
+    auto strips = [&](int cols) { return (g.N + cols - 1) / cols * kGradSplit; };
+    GradLayout l;
+    l.v8 = g.N % 8 == 0 && vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
+    // Strips of 64 columns where they give every SM two CTAs or the rows are few, else of 16 (6428 rows of 128 columns 13.4 -> 6.1 us, 20000
+    // of 33 116 -> 44; but 512 of 1024 3.4 -> 4.6).
+    l.wide = strips(kGradCols) >= 2 * sms || g.M < 1000;
+    l.grid = static_cast<int>(strips(l.wide ? kGradCols : kNarrowCols));   // (at most 2^29)
+    return l;
+}
+
 // ---- rows onto 16-byte boundaries --------------------------------------------------------------------------------------------
 // For operands whose rows start anywhere: the tensor-core kernels load tiles by TMA, which takes 16-byte boundaries only.  A copy costs
 // 4 bytes a value once, where a product reads the operand's tiles many times.  All of a call's operands in one launch; two aligned pieces
@@ -395,15 +414,12 @@ double lat_cost(const DenseGemm* g, int n, int sms, DenseLatChoice* best) {
     return least;
 }
 double pair_cost(const DenseGemm* g, int n, int sms, int bn) {
-    int64_t tiles = 0;
     double off = 0.0, bytes = 0.0;
     for (int j = 0; j < n; j++) {
-        tiles += ceil_div(g[j].M, 256) * ceil_div(g[j].N, g[j].gated ? bn / 2 : bn) * g[j].groups;
         off += (off_lines(g[j].a) + off_lines(g[j].b)) / n;
         bytes += gemm_bytes(g[j]);
     }
-    int rest, few, many;
-    const double chunks = dense_pair_share(g, n, bn, static_cast<int>(std::min<int64_t>(tiles, std::max(1, sms / 2))), &rest, &few, &many);
+    const double chunks = dense_pair_share(g, n, bn, sms).chunks;
     if (chunks < 0) return -1.0;
     // (two products side by side share less of what they load, as measured over 112 pairs of gradients)
     const double apart = n > 1 ? (bn == 256 ? 1.05 : 1.15) : 1.0;
@@ -426,31 +442,77 @@ GemmPlan plan_gemm(const DenseGemm* g, int n, int sms) {
     if (lat >= 0 && (best.us < 0 || lat < best.us)) best = GemmPlan{lat, true, 0, c};
     return best;
 }
-int launch_plan(const GemmPlan& p, const DenseGemm* g, int n, cudaStream_t s) {
-    if (p.us < 0) return DLF_E_UNSUPPORTED;
-    return p.lat ? launch_dense_lat(g, n, p.c, s) : launch_dense_pair(g, n, p.bn, s);
-}
-int launch_gemm(const DenseGemm& g, cudaStream_t s) {
-    int sms = 0;
-    const int rc = query_sms(&sms);
-    return rc ? rc : launch_plan(plan_gemm(&g, 1, sms), &g, 1, s);
-}
-// The gradients of an input and of weights: as one launch where its tiles fill the chip better than two launches' (4096 x 4096 x 4096:
-// 186 -> 171 us; 200 x 2048 x 1000, with the bias's: 15.1 -> 11.2), else one after the other.
-int launch_grads(DenseGemm* g, int n, cudaStream_t s) {
-    if (n == 0) return DLF_OK;
-    if (n == 1) return launch_gemm(g[0], s);
-    int sms = 0;
-    int rc = query_sms(&sms);
-    if (rc) return rc;
-    if (g[0].K * g[0].sources < g[1].K * g[1].sources) std::swap(g[0], g[1]);   // the longer tiles first, the shorter ones fill up
-    const GemmPlan one[2] = {plan_gemm(&g[0], 1, sms), plan_gemm(&g[1], 1, sms)}, both = plan_gemm(g, 2, sms);
-    if (both.us >= 0 && both.us < one[0].us + one[1].us) return launch_plan(both, g, 2, s);
-    rc = launch_plan(one[0], &g[0], 1, s);
-    return rc ? rc : launch_plan(one[1], &g[1], 1, s);
-}
+// What a call would do, asked for without doing it: the workspace that it wants, or the kernels that it launches, in their order.
+struct Ask {
+    size_t* workspace;
+    char* text;   // (null: the workspace is asked for)
+    size_t bytes, used;
+    int sms;
+    int say(const char* format, ...) {
+        const char* const between = used ? "; " : "";
+        if (used < bytes) used += static_cast<size_t>(std::snprintf(text + used, bytes - used, "%s", between));
+        va_list args;
+        va_start(args, format);
+        if (used < bytes) used += static_cast<size_t>(std::max(0, std::vsnprintf(text + used, bytes - used, format, args)));
+        va_end(args);
+        return DLF_OK;
+    }
+};
 
-// An operand as the products read it: itself, or a copy in the workspace (`run`: made now).
+// A call's launches - or, asked for, their names and what the host chose about them.
+struct Steps {
+    cudaStream_t s;
+    Ask* ask;
+    int sms = 0;
+    int begin() {
+        if (ask) sms = ask->sms;
+        return sms > 0 ? DLF_OK : query_sms(&sms);
+    }
+    int pack(const DensePack* jobs, int n) {
+        if (n == 0) return DLF_OK;
+        return ask ? ask->say("dense_pack(matrices=%d)", n) : launch_dense_pack(jobs, n, sms, s);
+    }
+    int grad(const DenseGrad& g) {
+        if (!ask) return launch_dense_grad(g, sms, s);
+        const GradLayout l = grad_layout(g, sms);
+        return ask->say("dense_grad(rows=%s columns=%d)", l.v8 ? "aligned" : "anywhere", l.wide ? kGradCols : kNarrowCols);
+    }
+    int gemv(const DenseGemm& g) {
+        if (!ask) return launch_dense_gemv(g, sms, s);
+        const DenseGemvLayout l = dense_gemv_layout(g, sms);
+        return ask->say("dense_gemv(tokens=%d rows=%s blocks=%d split=%d)", g.M > 8 ? 16 : 8, l.any ? "anywhere" : "aligned", static_cast<int>(l.blocks), 1 << l.lg_ranks);
+    }
+    int plan(const GemmPlan& p, const DenseGemm* g, int n) {
+        if (p.us < 0) return DLF_E_UNSUPPORTED;
+        if (!ask) return p.lat ? launch_dense_lat(g, n, p.c, s) : launch_dense_pair(g, n, p.bn, sms, s);
+        auto whole = [&](const DenseGemm& q, const Mat& m) { return !m.p || (dense_rows16(m) && q.N % 8 == 0); };   // (rows leave or come in pieces of 16 bytes)
+        bool all = true;
+        for (int j = 0; j < n; j++)
+            for (const Mat& m : g[j].out) all = all && whole(g[j], m);
+        const char* const out = all ? "aligned" : "anywhere";
+        const char* const res = !g[0].res.p ? "none" : whole(g[0], g[0].res) ? "aligned" : "anywhere";
+        if (p.lat) return ask->say("dense_lat(products=%d columns=%d split=%d sources=%d out=%s residual=%s)", n, p.c.bn, p.c.split, g[0].sources, out, res);
+        const DensePairShare t = dense_pair_share(g, n, p.bn, sms);
+        return ask->say("dense_pair(products=%d columns=%d sources=%d groups=%d pairs=%d rest=%d few=%d many=%d out=%s residual=%s)", n, p.bn, g[0].sources,
+                        g[n - 1].groups, t.pairs, t.rest, t.few, t.many, out, res);
+    }
+    int gemm(const DenseGemm& g) { return plan(plan_gemm(&g, 1, sms), &g, 1); }
+    // The gradients of an input and of weights: as one launch where its tiles fill the chip better than two launches' (4096 x 4096 x 4096:
+    // 186 -> 171 us; 200 x 2048 x 1000, with the bias's: 15.1 -> 11.2), else one after the other.
+    int grads(DenseGemm* g, int n) {
+        if (n == 0) return DLF_OK;
+        if (n == 1) return gemm(g[0]);
+        if (g[0].K * g[0].sources < g[1].K * g[1].sources) std::swap(g[0], g[1]);   // the longer tiles first, the shorter ones fill up
+        const GemmPlan one[2] = {plan_gemm(&g[0], 1, sms), plan_gemm(&g[1], 1, sms)}, both = plan_gemm(g, 2, sms);
+        if (both.us >= 0 && both.us < one[0].us + one[1].us) return plan(both, g, 2);
+        const int rc = plan(one[0], &g[0], 1);
+        return rc ? rc : plan(one[1], &g[1], 1);
+    }
+    int zero(const Mat& m, int64_t rows, int64_t cols) { return ask ? DLF_OK : zero_matrix(m, rows, cols, s); }
+    int zero(float* p, int64_t n) { return ask ? DLF_OK : zero_vec(p, n, s); }
+};
+
+// An operand as the products read it: itself, or a copy in the workspace (one of `jobs`).
 struct Operands {
     Carver& carve;
     DensePack jobs[kMaxPacks];
@@ -461,11 +523,23 @@ struct Operands {
         jobs[n++] = DensePack{rows, cols, m, to};
         return to;
     }
-    int run(cudaStream_t s) const { return n ? launch_dense_pack(jobs, n, s) : DLF_OK; }
 };
 
-// ---- the four operators; with `need` they only say how much workspace they want ------------------------------------------------
-int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+// ---- the four operators; with `ask` they only say what they would do -----------------------------------------------------------
+// (Asked for the kernels: a workspace to lay out, at an address that nothing is read from.)
+unsigned char* base_of(void* ws, const Ask* ask) { return ask && ask->text ? reinterpret_cast<unsigned char*>(256) : static_cast<unsigned char*>(ws); }
+// What a call wants, once that is known; true if nothing else was asked for.
+bool only_workspace(const Ask* ask, size_t bytes) {
+    if (!ask || ask->text) return false;
+    *ask->workspace = bytes;
+    return true;
+}
+int ready(const Ask* ask, const void* ws, size_t bytes, size_t need, Steps* steps) {
+    const int rc = ask ? DLF_OK : check_workspace(ws, bytes, need);
+    return rc ? rc : steps->begin();
+}
+
+int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, Ask* ask) {
     if (!a) return DLF_E_INVALID_ARG;
     int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
     if (rc) return rc;
@@ -482,20 +556,24 @@ int linear(const dlf_linear_args* a, void* ws, size_t ws_bytes, cudaStream_t s, 
     g.out[1] = mat(a->z, a->m, a->n, a->ldz, false);
     if (mat.rc) return mat.rc;
     if (shared({a->y, a->z}, {a->x, a->w, a->bias}) || (a->res && (a->z == a->res || (a->y == a->res && a->m > 1 && a->ldy != a->ldres)))) return DLF_E_INVALID_ARG;
-    if (need) *need = 0;
-    if (a->m == 0) return DLF_OK;
-    if (dense_gemv_takes(g)) return need ? DLF_OK : launch_dense_gemv(g, s);
-    Carver carve{static_cast<unsigned char*>(ws)};
+    Steps steps{s, ask};
+    const bool few = dense_gemv_takes(g);
+    if (a->m == 0 || few) {
+        if (only_workspace(ask, 0) || a->m == 0) return DLF_OK;
+        rc = steps.begin();
+        return rc ? rc : steps.gemv(g);
+    }
+    Carver carve{base_of(ws, ask)};
     Operands op{carve};
     g.a[0] = op(g.a[0], a->m, a->k);
     g.b[0] = op(g.b[0], a->n, a->k);
-    if (need) { *need = carve.used; return DLF_OK; }
-    rc = check_workspace(ws, ws_bytes, carve.used);
-    if (rc == DLF_OK) rc = op.run(s);
-    return rc ? rc : launch_gemm(g, s);
+    if (only_workspace(ask, carve.used)) return DLF_OK;
+    rc = ready(ask, ws, ws_bytes, carve.used, &steps);
+    if (rc == DLF_OK) rc = steps.pack(op.jobs, op.n);
+    return rc ? rc : steps.gemm(g);
 }
 
-int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaStream_t s, Ask* ask) {
     if (!a) return DLF_E_INVALID_ARG;
     int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
     if (rc) return rc;
@@ -509,21 +587,22 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
     if (mat.rc) return mat.rc;
     if (shared({a->dx, a->dw, a->db, a->dz}, {a->x, a->w}) || shared({a->dx, a->dw, a->db}, {a->dy, has_act ? a->z : nullptr})) return DLF_E_INVALID_ARG;
     if (some && a->m > 1 && a->dz && ((a->dz == a->dy && a->lddz != a->lddy) || (has_act && a->dz == a->z && a->lddz != a->ldz))) return DLF_E_INVALID_ARG;
+    Steps steps{s, ask};
     if (!some) {
-        if (need) { *need = 0; return DLF_OK; }
-        rc = zero_matrix(dw, a->n, a->k, s);
-        return rc ? rc : zero_vec(db, a->n, s);
+        if (only_workspace(ask, 0)) return DLF_OK;
+        rc = steps.zero(dw, a->n, a->k);
+        return rc ? rc : steps.zero(db, a->n);
     }
-    Carver carve{static_cast<unsigned char*>(ws)};
+    Carver carve{base_of(ws, ask)};
     Operands op{carve};
     const Mat xo = dw.p ? op(x, a->m, a->k) : x, wo = dx.p ? op(w, a->n, a->k) : w;
     // dz, as the products read it: dy itself where nothing lies between, the caller's dz, or a matrix of its own
     const bool products = dx.p || dw.p;
     Mat dz{nullptr, 0};
     if (products) dz = !has_act && dense_rows16(dy) ? dy : dz_out.p && dense_rows16(dz_out) ? dz_out : carve.matrix(a->m, a->n);
-    if (need) { *need = carve.used; return DLF_OK; }
-    rc = check_workspace(ws, ws_bytes, carve.used);
-    if (rc == DLF_OK) rc = op.run(s);
+    if (only_workspace(ask, carve.used)) return DLF_OK;
+    rc = ready(ask, ws, ws_bytes, carve.used, &steps);
+    if (rc == DLF_OK) rc = steps.pack(op.jobs, op.n);
     if (rc) return rc;
     const bool own_dz = products && dz.p != dy.p;
     if (own_dz || dz_out.p || db) {
@@ -534,7 +613,7 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
         if (own_dz) d.d0 = dz;
         if (dz_out.p && dz_out.p != d.d0.p) d.d0c = dz_out;
         d.db0 = db;
-        rc = launch_dense_grad(d, s);
+        rc = steps.grad(d);
         if (rc) return rc;
     }
     DenseGemm g[2] = {};
@@ -555,10 +634,10 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
         q.a[0] = dz; q.b[0] = xo; q.a_mn = q.b_mn = true;
         q.out[0] = dw;
     }
-    return launch_grads(g, n, s);
+    return steps.grads(g, n);
 }
 
-int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, Ask* ask) {
     if (!a) return DLF_E_INVALID_ARG;
     int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
     if (rc) return rc;
@@ -578,21 +657,25 @@ int gated(const dlf_gated_args* a, void* ws, size_t ws_bytes, cudaStream_t s, si
     g.out[2] = mat(a->u, a->m, a->n, a->ldu, false);
     if (mat.rc) return mat.rc;
     if (shared({a->h, a->g, a->u}, {a->x, a->wg, a->wu, a->bg, a->bu})) return DLF_E_INVALID_ARG;
-    if (need) *need = 0;
-    if (a->m == 0) return DLF_OK;
-    if (dense_gemv_takes(g)) return need ? DLF_OK : launch_dense_gemv(g, s);
-    Carver carve{static_cast<unsigned char*>(ws)};
+    Steps steps{s, ask};
+    const bool few = dense_gemv_takes(g);
+    if (a->m == 0 || few) {
+        if (only_workspace(ask, 0) || a->m == 0) return DLF_OK;
+        rc = steps.begin();
+        return rc ? rc : steps.gemv(g);
+    }
+    Carver carve{base_of(ws, ask)};
     Operands op{carve};
     g.a[0] = op(g.a[0], a->m, a->k);
     g.b[0] = op(g.b[0], a->n, a->k);
     g.b[1] = op(g.b[1], a->n, a->k);
-    if (need) { *need = carve.used; return DLF_OK; }
-    rc = check_workspace(ws, ws_bytes, carve.used);
-    if (rc == DLF_OK) rc = op.run(s);
-    return rc ? rc : launch_gemm(g, s);
+    if (only_workspace(ask, carve.used)) return DLF_OK;
+    rc = ready(ask, ws, ws_bytes, carve.used, &steps);
+    if (rc == DLF_OK) rc = steps.pack(op.jobs, op.n);
+    return rc ? rc : steps.gemm(g);
 }
 
-int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStream_t s, size_t* need) {
+int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStream_t s, Ask* ask) {
     if (!a) return DLF_E_INVALID_ARG;
     int rc = check_sizes(a->dtype, a->act, a->m, a->k, a->n);
     if (rc) return rc;
@@ -613,23 +696,24 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     d.db1 = const_cast<float*>(mat.vec(a->dbu));
     if (mat.rc) return mat.rc;
     if (shared({a->dx, a->dwg, a->dwu, a->dbg, a->dbu}, {a->dh, a->x, a->wg, a->wu, a->g, a->u})) return DLF_E_INVALID_ARG;
+    Steps steps{s, ask};
     if (!some) {
-        if (need) { *need = 0; return DLF_OK; }
-        rc = zero_matrix(dwg, a->n, a->k, s);
-        if (!rc) rc = zero_matrix(dwu, a->n, a->k, s);
-        if (!rc) rc = zero_vec(d.db0, a->n, s);
-        return rc ? rc : zero_vec(d.db1, a->n, s);
+        if (only_workspace(ask, 0)) return DLF_OK;
+        rc = steps.zero(dwg, a->n, a->k);
+        if (!rc) rc = steps.zero(dwu, a->n, a->k);
+        if (!rc) rc = steps.zero(d.db0, a->n);
+        return rc ? rc : steps.zero(d.db1, a->n);
     }
-    Carver carve{static_cast<unsigned char*>(ws)};
+    Carver carve{base_of(ws, ask)};
     Operands op{carve};
     const Mat xo = any_dw ? op(x, a->m, a->k) : x, wgo = dx.p ? op(wg, a->n, a->k) : wg, wuo = dx.p ? op(wu, a->n, a->k) : wu;
     if (dx.p || dwg.p) d.d0 = carve.matrix(a->m, a->n);
     if (dx.p || dwu.p) d.d1 = carve.matrix(a->m, a->n);
-    if (need) { *need = carve.used; return DLF_OK; }
-    rc = check_workspace(ws, ws_bytes, carve.used);
-    if (rc == DLF_OK) rc = op.run(s);
+    if (only_workspace(ask, carve.used)) return DLF_OK;
+    rc = ready(ask, ws, ws_bytes, carve.used, &steps);
+    if (rc == DLF_OK) rc = steps.pack(op.jobs, op.n);
     if (rc) return rc;
-    rc = launch_dense_grad(d, s);
+    rc = steps.grad(d);
     if (rc) return rc;
     DenseGemm g[2] = {};
     int n = 0;
@@ -653,15 +737,12 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
             q.out[1] = dwu;
         }
     }
-    return launch_grads(g, n, s);
+    return steps.grads(g, n);
 }
 
 }  // namespace
 
-int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s) {
-    int sms = 0;
-    const int rc = query_sms(&sms);
-    if (rc) return rc;
+int launch_dense_pack(const DensePack* jobs, int n, int sms, cudaStream_t s) {
     PackParams p{};
     p.n = n;
     for (int i = 0; i < n; i++) {
@@ -673,20 +754,12 @@ int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s) {
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
-int launch_dense_grad(const DenseGrad& g, cudaStream_t s) {
-    auto vec = [](const Mat& m) { return !m.p || (aligned(16, m.p) && m.ld % 8 == 0); };
-    const bool v8 = g.N % 8 == 0 && vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
-    int sms = 0;
-    const int rc = query_sms(&sms);
-    if (rc) return rc;
-    // Strips of 64 columns where they give every SM two CTAs or the rows are few, else of 16 (6428 rows of 128 columns 13.4 -> 6.1 us, 20000
-    // of 33 116 -> 44; but 512 of 1024 3.4 -> 4.6).
-    const bool wide = ceil_div(g.N, kGradCols) * kGradSplit >= 2 * sms || g.M < 1000;
-    const int grid = static_cast<int>(ceil_div(g.N, wide ? kGradCols : kNarrowCols) * kGradSplit);   // (at most 2^29)
+int launch_dense_grad(const DenseGrad& g, int sms, cudaStream_t s) {
+    const GradLayout l = grad_layout(g, sms);
     GradFn fn = nullptr;
-    if (g.dtype == DLF_BF16) fn = v8 ? pick_grad<__nv_bfloat16, 8>(g.gated, wide, g.act) : pick_grad<__nv_bfloat16, 2>(g.gated, wide, g.act);
-    else fn = v8 ? pick_grad<__half, 8>(g.gated, wide, g.act) : pick_grad<__half, 2>(g.gated, wide, g.act);
-    const cudaError_t e = launch_kernel(fn, grid, kGradThreads, 0, s, g);
+    if (g.dtype == DLF_BF16) fn = l.v8 ? pick_grad<__nv_bfloat16, 8>(g.gated, l.wide, g.act) : pick_grad<__nv_bfloat16, 2>(g.gated, l.wide, g.act);
+    else fn = l.v8 ? pick_grad<__half, 8>(g.gated, l.wide, g.act) : pick_grad<__half, 2>(g.gated, l.wide, g.act);
+    const cudaError_t e = launch_kernel(fn, l.grid, kGradThreads, 0, s, g);
     return e == cudaSuccess ? DLF_OK : cuda_fail(e);
 }
 
@@ -714,21 +787,26 @@ int dlf_dense_debug_stall(int which, int limit_us, void* stream) {
     return which ? dlf::dense_lat_stall(ns, static_cast<cudaStream_t>(stream)) : dlf::dense_pair_stall(ns, static_cast<cudaStream_t>(stream));
 }
 
-int dlf_linear_workspace_bytes(const dlf_linear_args* a, size_t* bytes) { return bytes ? dlf::linear(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
-int dlf_linear(const dlf_linear_args* a, void* workspace_dev, size_t bytes, void* stream) {
-    return dlf::linear(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
-}
-int dlf_linear_grad_workspace_bytes(const dlf_linear_grad_args* a, size_t* bytes) { return bytes ? dlf::linear_grad(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
-int dlf_linear_grad(const dlf_linear_grad_args* a, void* workspace_dev, size_t bytes, void* stream) {
-    return dlf::linear_grad(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
-}
-int dlf_gated_workspace_bytes(const dlf_gated_args* a, size_t* bytes) { return bytes ? dlf::gated(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
-int dlf_gated(const dlf_gated_args* a, void* workspace_dev, size_t bytes, void* stream) {
-    return dlf::gated(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
-}
-int dlf_gated_grad_workspace_bytes(const dlf_gated_grad_args* a, size_t* bytes) { return bytes ? dlf::gated_grad(a, nullptr, 0, nullptr, bytes) : DLF_E_INVALID_ARG; }
-int dlf_gated_grad(const dlf_gated_grad_args* a, void* workspace_dev, size_t bytes, void* stream) {
-    return dlf::gated_grad(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);
-}
+// What a call would do: its workspace, its kernels.
+#define DLF_DENSE_ENTRIES(OP)                                                                                                  \
+    int dlf_##OP##_workspace_bytes(const dlf_##OP##_args* a, size_t* bytes) {                                                   \
+        if (!bytes) return DLF_E_INVALID_ARG;                                                                                   \
+        dlf::Ask ask{bytes, nullptr, 0, 0, 0};                                                                                  \
+        return dlf::OP(a, nullptr, 0, nullptr, &ask);                                                                           \
+    }                                                                                                                           \
+    int dlf_##OP##_kernels(const dlf_##OP##_args* a, int sm_count, char* text, size_t bytes) {                                  \
+        if (!text || bytes == 0 || sm_count < 0) return DLF_E_INVALID_ARG;                                                      \
+        text[0] = 0;                                                                                                            \
+        dlf::Ask ask{nullptr, text, bytes, 0, sm_count};                                                                        \
+        return dlf::OP(a, nullptr, 0, nullptr, &ask);                                                                           \
+    }                                                                                                                           \
+    int dlf_##OP(const dlf_##OP##_args* a, void* workspace_dev, size_t bytes, void* stream) {                                   \
+        return dlf::OP(a, workspace_dev, bytes, static_cast<cudaStream_t>(stream), nullptr);                                    \
+    }
+DLF_DENSE_ENTRIES(linear)
+DLF_DENSE_ENTRIES(linear_grad)
+DLF_DENSE_ENTRIES(gated)
+DLF_DENSE_ENTRIES(gated_grad)
+#undef DLF_DENSE_ENTRIES
 
 }  // extern "C"

@@ -47,8 +47,12 @@ inline bool dense_rows16(const Mat& m) { return aligned(16, m.p) && m.ld % 8 == 
 
 // Products `g[0]` to `g[n - 1]` as one launch: one forward product, or one or two gradients (b_mn).
 // dense_tc.cu: tiles of 256 rows by bn (256, 128; gated: 256, both halves) columns of B; operands with rows on 16-byte boundaries.
-int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s);
-double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest, int* few, int* many);   // chunks of K until the last pair is done
+int launch_dense_pair(const DenseGemm* g, int n, int bn, int sms, cudaStream_t s);
+struct DensePairShare {
+    double chunks;                // of K until the last pair is done; negative: no such share
+    int pairs, rest, few, many;   // (dense_tc.cu's PairParams)
+};
+DensePairShare dense_pair_share(const DenseGemm* g, int n, int bn, int sms);
 int dense_pair_gave_up(cudaStream_t s, int* count);           // waits for the stream; CTAs in which a bounded wait has given up so far
 int dense_pair_stall(unsigned long long limit_ns, cudaStream_t s);   // a wait that does
 // dense_lat.cu: tiles of at most 128 rows by `bn` columns of B (64, 128, forward 96, too; both halves of a gated tile), K shared out over `split` CTAs (1, 2,
@@ -63,7 +67,13 @@ int dense_lat_gave_up(cudaStream_t s, int* count);
 int dense_lat_stall(unsigned long long limit_ns, cudaStream_t s);
 
 bool dense_gemv_takes(const DenseGemm& g);                           // dense_gemv.cu: forward products of a few tokens, any rows
-int launch_dense_gemv(const DenseGemm& g, cudaStream_t s);
+struct DenseGemvLayout {
+    bool any;               // rows anywhere
+    int rows, lg_ranks;     // weight rows of a CTA; CTAs that share their K
+    int64_t groups, blocks; // CTAs without such a share; blocks of K of a CTA before it
+};
+DenseGemvLayout dense_gemv_layout(const DenseGemm& g, int sms);
+int launch_dense_gemv(const DenseGemm& g, int sms, cudaStream_t s);
 
 // Copies matrices to rows on 16-byte boundaries (zeros behind a row's end, up to the boundary).
 constexpr int kMaxPacks = 3;   // (x and both weight matrices)
@@ -71,7 +81,7 @@ struct DensePack {
     int64_t rows, cols;
     Mat from, to;
 };
-int launch_dense_pack(const DensePack* jobs, int n, cudaStream_t s);
-int launch_dense_grad(const DenseGrad& g, cudaStream_t s);
+int launch_dense_pack(const DensePack* jobs, int n, int sms, cudaStream_t s);
+int launch_dense_grad(const DenseGrad& g, int sms, cudaStream_t s);
 
 }  // namespace dlf

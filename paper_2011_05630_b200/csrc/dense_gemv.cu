@@ -246,31 +246,40 @@ bool dense_gemv_takes(const DenseGemm& g) {
     return !g.gated || same(g.b[0], g.b[1]);
 }
 
-int launch_dense_gemv(const DenseGemm& g, cudaStream_t s) {
-    int sms = 0;
-    const int rc = query_sms(&sms);
-    if (rc) return rc;
-    const bool any = g.K % 8 != 0 || !dense_rows16(g.a[0]) || !dense_rows16(g.b[0]) || !dense_rows16(g.b[1]);
+DenseGemvLayout dense_gemv_layout(const DenseGemm& g, int sms) {
+    DenseGemvLayout l;
+    l.any = g.K % 8 != 0 || !dense_rows16(g.a[0]) || !dense_rows16(g.b[0]) || !dense_rows16(g.b[1]);
+    const int64_t classes = l.any ? 8 : 1, per_class = (g.N + classes - 1) / classes;
+    l.rows = static_cast<int>(std::max<int64_t>(8, (g.N + 2 * sms - 1) / (2 * sms)));
+    l.groups = classes * ((per_class + l.rows - 1) / l.rows);
+    // Few rows: their K is shared out over the CTAs of a cluster where there is room for them and enough work: a block of a warp's steps
+    // takes about 0.8 us, meeting in a cluster 1.7 (10094 -> 624, gated, one token: 16 -> 12 us; 2048 -> 1000: 3.4 -> 4.3, not done).
+    const int64_t block = kWarps * 32 * steps_ahead(g.M > 8 ? 2 : 1, g.gated, l.any);
+    l.blocks = (g.K + block - 1) / block;
+    l.lg_ranks = 0;
+    double least = 0.8 * static_cast<double>(l.blocks);
+    for (int lg = 1; lg <= 3 && (l.groups << lg) <= 2 * sms; lg++) {
+        const double us = 0.8 * static_cast<double>((l.blocks + (1 << lg) - 1) >> lg) + 1.7;
+        if (us < least) {
+            least = us;
+            l.lg_ranks = lg;
+        }
+    }
+    return l;
+}
+
+int launch_dense_gemv(const DenseGemm& g, int sms, cudaStream_t s) {
+    const DenseGemvLayout l = dense_gemv_layout(g, sms);
+    const bool any = l.any;
+    const int64_t groups = l.groups;
     GemvParams p{};
     p.x = g.a[0];
     for (int i = 0; i < 2; i++) { p.w[i] = g.b[i]; p.bias[i] = g.bias[i]; }
     for (int i = 0; i < 3; i++) p.o[i] = g.out[i];
     p.res = g.res;
     p.N = g.N; p.M = static_cast<int>(g.M); p.K = static_cast<int>(g.K); p.act = g.act;
-    const int64_t classes = any ? 8 : 1, per_class = (g.N + classes - 1) / classes;
-    p.rows = static_cast<int>(std::max<int64_t>(8, (g.N + 2 * sms - 1) / (2 * sms)));
-    const int64_t groups = classes * ((per_class + p.rows - 1) / p.rows);
-    // Few rows: their K is shared out over the CTAs of a cluster where there is room for them and enough work: a block of a warp's steps
-    // takes about 0.8 us, meeting in a cluster 1.7 (10094 -> 624, gated, one token: 16 -> 12 us; 2048 -> 1000: 3.4 -> 4.3, not done).
-    const int64_t block = kWarps * 32 * steps_ahead(g.M > 8 ? 2 : 1, g.gated, any), blocks = (g.K + block - 1) / block;
-    double least = 0.8 * static_cast<double>(blocks);
-    for (int lg = 1; lg <= 3 && (groups << lg) <= 2 * sms; lg++) {
-        const double us = 0.8 * static_cast<double>((blocks + (1 << lg) - 1) >> lg) + 1.7;
-        if (us < least) {
-            least = us;
-            p.lg_ranks = lg;
-        }
-    }
+    p.rows = l.rows;
+    p.lg_ranks = l.lg_ranks;
     const int ranks = 1 << p.lg_ranks;
     const bool bf = g.dtype == DLF_BF16;
     const GemvFn fn = g.M > 8 ? (bf ? pick_gemv<__nv_bfloat16, 2>(g.gated, any) : pick_gemv<__half, 2>(g.gated, any))

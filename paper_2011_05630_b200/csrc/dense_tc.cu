@@ -458,17 +458,19 @@ int launch_grads(int bn, const PairParams<2>& p, cudaStream_t s) {
 
 // How the pairs share two jobs' tiles (see PairParams): the least time, in chunks of K, by which every tile has a pair.  Tiles of the second
 // job go to the pairs with one tile less of the first until they are as late as the others.
-double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest, int* few, int* many) {
+DensePairShare dense_pair_share(const DenseGemm* g, int n, int bn, int sms) {
     // (a tile's rows take as long as 8 chunks, 2.4 of them before its accumulator is free again)
     auto tiles = [&](const DenseGemm& q) { return ((q.M + 255) / 256) * ((q.N + (q.gated ? bn / 2 : bn) - 1) / (q.gated ? bn / 2 : bn)) * q.groups; };
     auto cost = [&](const DenseGemm& q) { return static_cast<double>((q.K + 63) / 64 * q.sources) + 2.4; };
     const int64_t t0 = tiles(g[0]), t1 = n > 1 ? tiles(g[1]) : 0;
+    const int pairs = static_cast<int>(std::min<int64_t>(t0 + t1, std::max(1, sms / 2)));
     const int64_t q0 = t0 / pairs, r = t0 % pairs;
-    *rest = static_cast<int>(r);
-    *few = *many = 0;
-    const double c0 = cost(g[0]);
-    double end = c0 * static_cast<double>(q0 + (r ? 1 : 0));
-    if (t1 == 0) return end;
+    DensePairShare share{-1.0, pairs, static_cast<int>(r), 0, 0};
+    const double c0 = cost(g[0]), end = c0 * static_cast<double>(q0 + (r ? 1 : 0));
+    if (t1 == 0) {
+        share.chunks = end;
+        return share;
+    }
     const double c1 = cost(g[1]);
     // the earliest end at which the places suffice, from the perfectly even one on
     double T = (c0 * static_cast<double>(t0) + c1 * static_cast<double>(t1)) / pairs;
@@ -476,19 +478,20 @@ double dense_pair_share(const DenseGemm* g, int n, int bn, int pairs, int* rest,
         const int64_t few_n = std::max<int64_t>(0, static_cast<int64_t>((T - c0 * static_cast<double>(q0)) / c1 + 1e-9));
         const int64_t many_n = std::max<int64_t>(0, static_cast<int64_t>((T - c0 * static_cast<double>(q0 + 1)) / c1 + 1e-9));
         if (few_n * (pairs - r) + many_n * r >= t1) {
-            *few = static_cast<int>(few_n);
-            *many = static_cast<int>(many_n);
-            return std::max(end, T);
+            share.few = static_cast<int>(few_n);
+            share.many = static_cast<int>(many_n);
+            share.chunks = std::max(end, T);
+            return share;
         }
         T += c1 / 8;
     }
-    return -1.0;
+    return share;
 }
 
-int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s) {
-    int sms = 0;
-    int rc = query_sms(&sms);
-    if (rc) return rc;
+int launch_dense_pair(const DenseGemm* g, int n, int bn, int sms, cudaStream_t s) {
+    int rc = DLF_OK;
+    const DensePairShare share = dense_pair_share(g, n, bn, sms);
+    if (share.chunks < 0) return DLF_E_UNSUPPORTED;
     const bool bf = g[0].dtype == DLF_BF16;
     if (!g[0].b_mn) {
         PairParams<1> p;
@@ -499,19 +502,17 @@ int launch_dense_pair(const DenseGemm* g, int n, int bn, cudaStream_t s) {
         p.res_vec = dense_rows16(g[0].res);
         p.bias[0] = g[0].bias[0]; p.bias[1] = g[0].bias[1];
         p.act = g[0].act;
-        p.pairs = static_cast<int>(std::min<long long>(p.job[0].tiles, std::max(1, sms / 2)));
+        p.pairs = share.pairs;
         return bf ? launch_forward<__nv_bfloat16>(g[0], bn, p, s) : launch_forward<__half>(g[0], bn, p, s);
     }
     PairParams<2> p;
     std::memset(&p, 0, sizeof(p));
-    long long tiles = 0;
     for (int i = 0; i < n; i++) {
         rc = fill_job(g[i], bn, &p.job[i]);
         if (rc) return rc;
-        tiles += p.job[i].tiles;
     }
-    p.pairs = static_cast<int>(std::min<long long>(tiles, std::max(1, sms / 2)));
-    if (dense_pair_share(g, n, bn, p.pairs, &p.rest, &p.few, &p.many) < 0) return DLF_E_UNSUPPORTED;
+    p.pairs = share.pairs;
+    p.rest = share.rest; p.few = share.few; p.many = share.many;
     return bf ? launch_grads<__nv_bfloat16>(bn, p, s) : launch_grads<__half>(bn, p, s);
 }
 
