@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import threading
 
 import torch
 
@@ -26,6 +27,7 @@ _LINEAR_GRAD = struct.Struct("@ii3q8P7q")
 _GATED = struct.Struct("@ii3q8P6q")
 _GATED_GRAD = struct.Struct("@ii3q11P9q")
 _ops = {}   # name -> (call, its workspace query)
+_heard = threading.local()   # .texts: a list, while `kernels` listens in this thread
 
 
 def _enter(x, act, *others):
@@ -95,6 +97,21 @@ def _call(op, args, like, ask):
         status = fns[0](args, ws.data_ptr() if need.value else None, need.value, stream)
     if status != B.OK:
         raise B.DlfError(status, op)
+    texts = getattr(_heard, "texts", None)
+    if texts is not None:
+        text = C.create_string_buffer(1024)
+        B._check(getattr(B.lib(), op + "_kernels")(args, 0, text, len(text)), op)
+        texts.append(text.value.decode())
+
+
+def kernels(call):
+    """Makes the call (a function without arguments) and says what its dense operators launched: a text for each (see dlf_linear_kernels)."""
+    before, _heard.texts = getattr(_heard, "texts", None), []
+    try:
+        call()
+        return _heard.texts
+    finally:
+        _heard.texts = before
 
 
 def synchronize(device=None):

@@ -12,7 +12,7 @@ group's input to its last layer; --group-kernel picks the hand-over (1 shared me
 --op dwconv runs a depthwise KxK layer (COUT = CIN), --op maxpool a KxK max-pool; --mbconv HID runs the fused
 inverted-residual block CIN -> HID (1x1) -> depthwise 3x3 (--stride) -> COUT (1x1) as one group.
 --op linear runs the dense operator act(x w^T + bias [+ residual]) on N*H*W tokens of CIN -> COUT values (K is not used), --op gated the gated
-block's act(x wg^T) * (x wu^T), --backward their gradients, too; each prints its time on the device.
+block's act(x wg^T) * (x wu^T), --backward their gradients, too; each prints its time on the device and the kernels that ran.
 """
 from __future__ import annotations
 
@@ -36,7 +36,7 @@ def dense_op(a):
         calls["backward"] = ((lambda: dense.linear_backward(dy, x, w, kept[1], act=act, residual=a.residual)) if a.op == "linear"
                              else (lambda: dense.gated_backward(dy, x, w, wu, kept[1], kept[2], act=act)))
     for name, call in calls.items():
-        call()
+        ran, = dense.kernels(call)
         ends = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
         ends[0].record()
         for _ in range(a.reps):
@@ -44,6 +44,7 @@ def dense_op(a):
         ends[1].record()
         dense.synchronize()
         print("%s %s, %d tokens of %d -> %d, %s, act %s: %.2f us a call, x %d" % (a.op, name, m, k, n, a.dtype, act, ends[0].elapsed_time(ends[1]) * 1e3 / a.reps, a.reps))
+        print("  " + ran)
 
 
 def main():
