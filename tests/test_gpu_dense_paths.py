@@ -31,7 +31,7 @@ class Matrix:
 def run(case, dtype, values, act=None):
     """(inputs, outputs) of a call: values(rows, cols, name) makes an input."""
     outs = P.OUTPUTS[case.op].split()
-    case = P.Case(case.name, case.op, case.m, case.k, case.n, case.expect, "", case.pad, case.shift, case.out_pad, case.out_shift, act or case.act)
+    case = P.Case(case.name, case.op, case.m, case.k, case.n, case.expect, " ".join(case.without), case.pad, case.shift, case.out_pad, case.out_shift, act or case.act)
     mats = {t: Matrix(*size, GUARD if t in outs else float("nan"), dtype) for t, size in case.matrices().items()}
     vecs = {t: torch.full((case.n + 17,), GUARD, device="cuda") for t in case.vectors()}
     vec = lambda t: vecs[t][1:1 + case.n]   # (off the 16-byte boundaries)
@@ -65,11 +65,11 @@ def formulas(op, v, a):
     """The outputs in 64 bits, and how far fp32 sums and 16-bit operands may be off: name -> (value, slack)."""
     t = {name: x.double() for name, x in v.items()}
     if op == "linear":
-        z, s, y, ys = D.linear_ref(v["x"], v["w"], v["bias"], v["res"], a)
+        z, s, y, ys = D.linear_ref(v["x"], v["w"], v.get("bias"), v.get("res"), a)
         return {"z": (z, s), "y": (y, ys)}
     if op == "gated":
-        g, gs, h, hs = D.linear_ref(v["x"], v["wg"], v["bg"], None, a)
-        u, us, _, _ = D.linear_ref(v["x"], v["wu"], v["bu"], None, "none")
+        g, gs, h, hs = D.linear_ref(v["x"], v["wg"], v.get("bg"), None, a)
+        u, us, _, _ = D.linear_ref(v["x"], v["wu"], v.get("bu"), None, "none")
         return {"g": (g, gs), "u": (u, us), "h": (h * u, h.abs() * us + hs * u.abs() + hs * us + 2.0 ** -23 * (h * u).abs())}
     m, dtype = v["x"].shape[0], v["x"].dtype
     if op == "linear_grad":
@@ -119,3 +119,61 @@ def test_the_device_gets_what_the_cases_are_for():
         pytest.skip("the cases' words are for 148 SMs")
     for c in P.CASES:
         assert c.on_host(0) == c.on_host(148)
+
+
+WITHOUT = {"linear": ["bias", "res", "z", "bias res z"], "gated": ["bg", "bu", "g", "u", "bg bu g u"],
+           "linear_grad": ["dx", "dw", "db", "dz", "dx db", "dw dz", "dx dw", "dx dw db", "dx dw dz", "dx dw db dz"],
+           "gated_grad": ["dx", "dwg", "dwu", "dbg", "dbu", "dx dwg", "dx dwu", "dwg dwu", "dwg dbg", "dwu dbu", "dx dwg dwu", "dx dwg dwu dbg", "dx dwg dwu dbg dbu"]}
+
+
+@pytest.mark.parametrize("op", list(P.STRUCTS))
+@pytest.mark.parametrize("size", [(5, 200, 104), (130, 72, 264), (1500, 264, 520), (7, 129, 33), (1100, 65, 43)], ids=str)
+def test_what_is_left_out(size, op):
+    """Every optional matrix and vector is null once: the others are what they are with it."""
+    for without in WITHOUT[op]:
+        for out_pad, pad in ((0, 0), (3, 1)):
+            gen = torch.Generator(device="cuda").manual_seed(sum(size))
+            c = P.Case("without " + without, op, *size, "", without, pad=pad, out_pad=out_pad)
+            given, got = run(c, torch.bfloat16, lambda r, q, name: torch.randint(-2, 3, (r, q), generator=gen, device="cuda").float())
+            for name, (want, _) in formulas(op, given, c.act).items():
+                assert (name in got) == (name not in c.without)
+                if name in got:
+                    assert torch.equal(got[name], want.to(got[name].dtype)), (without, name, c.on_host(0))
+
+
+@pytest.mark.parametrize("size", [(200, 136, 264), (3001, 40, 33), (90, 33, 57), (2500, 24, 130)], ids=str)
+@pytest.mark.parametrize("place", ["dy", "z"])
+def test_dz_in_the_place_of_an_input(size, place):
+    """dz over dy or over z, in rows on the 16-byte boundaries and off them, wide strips and narrow ones."""
+    m, k, n = size
+    for pad in (0, 1):
+        gen = torch.Generator(device="cuda").manual_seed(m)
+        c = P.Case("", "linear_grad", m, k, n, "", pad=pad, out_pad=pad, act="relu")
+        whole = lambda r, q: torch.randint(-2, 3, (r, q), generator=gen, device="cuda").float()
+        mats = {t: Matrix(*s, GUARD if t in ("dx", "dw") else float("nan"), torch.float16) for t, s in c.matrices().items() if t != "dz"}
+        for t in ("dy", "x", "w", "z"):
+            mats[t].t.copy_(whole(*mats[t].t.shape))
+        given, db = {t: mats[t].t.clone() for t in ("dy", "x", "w", "z")}, torch.zeros(n, device="cuda")
+        mats["dz"] = mats[place]
+        args = c.pack("f16", lambda t: db.data_ptr() if t == "db" else mats[t].t.data_ptr())
+        need = C.c_size_t()
+        B._check(B.lib().dlf_linear_grad_workspace_bytes(args, C.byref(need)), "")
+        ws = torch.empty(max(1, need.value), device="cuda", dtype=torch.uint8)
+        B._check(B.lib().dlf_linear_grad(args, ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream), "dlf_linear_grad")
+        got = {"dx": mats["dx"].t, "dw": mats["dw"].t, "dz": mats["dz"].t, "db": db}
+        for name, (want, _) in formulas("linear_grad", given, "relu").items():
+            assert torch.equal(got[name], want.to(got[name].dtype)), (name, pad)
+    dense.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["float16", "bfloat16"])
+@pytest.mark.parametrize("op", list(P.STRUCTS))
+@pytest.mark.parametrize("size", [(1, 200000, 72), (40, 100000, 64), (100000, 64, 40), (70, 72, 100000), (33, 20001, 35), (20001, 35, 33), (35, 33, 20001)], ids=str)
+def test_long_and_thin(size, op, dtype):
+    """One size far above the others: sums of many terms, many strips, a single tile."""
+    gen = torch.Generator(device="cuda").manual_seed(sum(size))
+    c = P.Case(str(size), op, *size, "")
+    given, got = run(c, dtype, lambda r, q, name: torch.randint(-2, 3, (r, q), generator=gen, device="cuda").float())
+    for name, (want, _) in formulas(op, given, c.act).items():
+        assert float(want.abs().max()) < 2 ** 24
+        assert torch.equal(got[name], want.to(got[name].dtype)), (name, c.on_host(0))
