@@ -27,10 +27,10 @@ _LINEAR_GRAD = struct.Struct("@ii3q8P7q")
 _GATED = struct.Struct("@ii3q8P6q")
 _GATED_GRAD = struct.Struct("@ii3q11P9q")
 _ops = {}   # name -> (call, its workspace query)
-_heard = threading.local()   # .texts: a list, while `kernels` listens in this thread
+_heard = {}   # thread -> list, while `kernels` listens there (a thread-local variable costs every call 0.4 us)
 
 
-def _enter(x, act, *others):
+def _enter(x, act, *tensors):
     """What a call's first matrix and its activation are to the library, once nothing speaks against the call as such."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("a CUDA tensor is required: there is no CPU path")
@@ -42,7 +42,7 @@ def _enter(x, act, *others):
     if x.dim() != 2:
         raise ValueError("matrices have two dimensions, got %d" % x.dim())
     if torch.is_grad_enabled():
-        for t in (x, *others):
+        for t in tensors:
             if t is not None and t.requires_grad:
                 raise ValueError("a tensor requires a gradient, and nothing would be recorded for it: call under torch.no_grad(), or with detached tensors")
     return dtype, a
@@ -50,9 +50,10 @@ def _enter(x, act, *others):
 
 def _size(t, name, i):
     """Rows (i 0) or columns (1) of what has to be a matrix."""
-    if t.dim() != 2:
-        raise ValueError("%s: matrices have two dimensions, got %d" % (name, t.dim()))
-    return t.shape[i]
+    try:
+        return t.shape[i]
+    except IndexError:
+        raise ValueError("%s: matrices have two dimensions, got %d" % (name, t.dim())) from None
 
 
 def _mat(t, name, shape, like):
@@ -97,21 +98,25 @@ def _call(op, args, like, ask):
         status = fns[0](args, ws.data_ptr() if need.value else None, need.value, stream)
     if status != B.OK:
         raise B.DlfError(status, op)
-    texts = getattr(_heard, "texts", None)
-    if texts is not None:
+    if _heard and threading.get_ident() in _heard:
         text = C.create_string_buffer(1024)
         B._check(getattr(B.lib(), op + "_kernels")(args, 0, text, len(text)), op)
-        texts.append(text.value.decode())
+        _heard[threading.get_ident()].append(text.value.decode())
 
 
 def kernels(call):
     """Makes the call (a function without arguments) and says what its dense operators launched: a text for each (see dlf_linear_kernels)."""
-    before, _heard.texts = getattr(_heard, "texts", None), []
+    me, texts = threading.get_ident(), []
+    before = _heard.get(me)
+    _heard[me] = texts
     try:
         call()
-        return _heard.texts
     finally:
-        _heard.texts = before
+        if before is None:
+            del _heard[me]
+        else:
+            _heard[me] = before
+    return texts
 
 
 def synchronize(device=None):
@@ -123,7 +128,7 @@ def synchronize(device=None):
 def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
     """y = act(x w^T + bias + residual) for x [m][k], w [n][k], residual [m][n]; with `save` (y, z), z being the sum that the
     activation was applied to.  `out` receives y and may be the residual itself."""
-    dtype, a = _enter(x, act, w, bias, residual, out)
+    dtype, a = _enter(x, act, x, w, bias, residual, out)
     m, k = x.shape
     n = _size(w, "w", 0)
     xp, ldx = _mat(x, "x", (m, k), x)
@@ -140,7 +145,7 @@ def linear(x, w, bias=None, residual=None, act="none", save=False, out=None):
 def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, need_dx=True, need_dw=True):
     """(dx, dw, db, dr): the gradients of `linear`'s inputs, None for one that is not asked for.  z: what `linear(..., save=True)`
     kept, needed with an activation.  dr, the residual's gradient, is dy itself where there is no activation."""
-    dtype, a = _enter(dy, act, x, w, z)
+    dtype, a = _enter(dy, act, dy, x, w, z)
     m, n = dy.shape
     k = _size(x, "x", 1) if x is not None else _size(w, "w", 1) if w is not None else 1
     if a and z is None:
@@ -163,7 +168,7 @@ def linear_backward(dy, x, w, z=None, act="none", bias=True, residual=False, nee
 
 def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
     """h = act(x wg^T + bg) * (x wu^T + bu) for x [m][k], wg and wu [n][k]; with `save` (h, g, u), g and u being the two sums."""
-    dtype, a = _enter(x, act, wg, wu, bg, bu, out)
+    dtype, a = _enter(x, act, x, wg, wu, bg, bu, out)
     m, k = x.shape
     n = _size(wg, "wg", 0)
     xp, ldx = _mat(x, "x", (m, k), x)
@@ -181,7 +186,7 @@ def gated(x, wg, wu, bg=None, bu=None, act="silu", save=False, out=None):
 def gated_backward(dh, x, wg, wu, g, u, act="silu", bias=False, need_dx=True, need_dw=True):
     """(dx, dwg, dwu, dbg, dbu): the gradients of `gated`'s inputs, None for one that is not asked for.  g and u: what
     `gated(..., save=True)` kept."""
-    dtype, a = _enter(dh, act, x, wg, wu, g, u)
+    dtype, a = _enter(dh, act, dh, x, wg, wu, g, u)
     m, n = dh.shape
     k = _size(x, "x", 1) if x is not None else _size(wg, "wg", 1) if wg is not None else 1
     if (need_dw and x is None) or (need_dx and (wg is None or wu is None)) or g is None or u is None:
