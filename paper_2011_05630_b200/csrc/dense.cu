@@ -26,16 +26,12 @@ namespace {
 // the same bits every time, no atomics and no second kernel.
 constexpr int kGradCols = 64, kNarrowCols = 16, kGradThreads = 128, kGradSplit = 8;
 
-// V values of a row, as they lie in memory: 8 on a 16-byte boundary, or 2 anywhere; `n` of them exist (of 8 all or none).
+// V values of a row, as they lie in memory: 8 on a 16-byte boundary (they come through shared memory), or 2 anywhere, n of which exist.
 template <typename T, int V>
 struct Run;
 template <typename T>
 struct Run<T, 8> {
     uint4 q;
-    __device__ __forceinline__ void load(const Mat& m, int64_t row, int64_t col, int n) {
-        q = make_uint4(0u, 0u, 0u, 0u);
-        if (n) q = ld_map(reinterpret_cast<const uint4*>(static_cast<const T*>(m.p) + row * m.ld + col));
-    }
     __device__ __forceinline__ float2 get2(int i) const { return unpack2<T>(i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w); }
     __device__ __forceinline__ void set2(int i, float2 f) { (i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w) = pack2<T>(f.x, f.y); }
     __device__ __forceinline__ void store(const Mat& m, int64_t row, int64_t col, int) const {
