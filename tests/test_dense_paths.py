@@ -54,3 +54,10 @@ def test_the_answer_goes_with_the_workspace(op):
         B._check(getattr(B.lib(), "dlf_%s_workspace_bytes" % op)(c.pack("bf16", at.get), C.byref(need)), op)
         names = [part.split("(")[0] for part in P.parts(c.on_host())]
         assert (need.value > 0) == ("dense_pack" in names or (op.endswith("grad") and not (op == "linear_grad" and (c.out_pad + c.n) % 8 == 0 and c.out_shift % 8 == 0))), c.name
+
+
+@pytest.mark.parametrize("sms", [1, 2, 3, 20, 132, 148, 160])
+def test_any_number_of_sms_has_an_answer(sms):
+    for c in P.CASES:
+        names = [part.split("(")[0] for part in P.parts(c.on_host(sms))]
+        assert names and not set(names) - {"dense_gemv", "dense_lat", "dense_pair", "dense_grad", "dense_pack"}, (c.name, sms)
