@@ -106,7 +106,8 @@ __global__ void __cluster_dims__(kGradSplit, 1, 1) __launch_bounds__(kGradThread
     if constexpr (V == 8) {
         // a thread's next rows come into places of its own in shared memory (nobody else's: nothing to meet for), kAhead - 1 rows ahead
         // of the one worked on: 16 KB of places for a CTA, 24 gated, without a register for them.  Against two rows ahead in registers,
-        // 4096 x 5632: GELU with its gradient written 32.5 -> 29.4 us, gated with the sums alone 38.3 -> 25.5; six places 30.1 and 28.7.
+        // 4096 x 5632: GELU with its gradient written 32.5 -> 29.4 us (30.9 with normal2 as it is now), SILU gated with the sums alone
+        // 38.3 -> 25.5; six places 30.1 and 28.7.
         constexpr int kAhead = 4, kArrays = GATED ? 3 : kWithZ ? 2 : 1;
         __shared__ uint4 ring[kAhead][kArrays][kGradThreads];
         auto fetch = [&](int64_t row, int slot) {
@@ -236,8 +237,9 @@ GradLayout grad_layout(const DenseGrad& g, int sms) {
     auto strips = [&](int cols) { return (g.N + cols - 1) / cols * kGradSplit; };
     GradLayout l;
     l.v8 = g.N % 8 == 0 && vec(g.dy) && vec(g.z) && vec(g.u) && vec(g.d0) && vec(g.d1) && vec(g.d0c);
-    // Strips of 64 columns where they give every SM two CTAs or the rows are few, else of 16 (6428 rows of 128 columns 13.4 -> 6.1 us, 20000
-    // of 33 116 -> 44; but 512 of 1024 3.4 -> 4.6).
+    // Strips of 64 columns where they give every SM two CTAs or the rows are few, else of 16.  GELU with its gradient written, wide -> narrow:
+    // 1000 rows of 128 3.6 -> 2.6 us, 6428 of 128 12.0 -> 4.7, 20000 of 33 127 -> 36; but 512 of 1024 3.3 -> 4.1.  (Between the two the rule is up to
+    // 2 us off, 2048 of 2048 7.8 -> 9.6, and below 1000 rows more where they are off the boundaries: 900 of 130 7.8 -> 3.6.)
     l.wide = strips(kGradCols) >= 2 * sms || g.M < 1000;
     l.grid = static_cast<int>(strips(l.wide ? kGradCols : kNarrowCols));   // (at most 2^29)
     return l;
@@ -592,7 +594,9 @@ int linear_grad(const dlf_linear_grad_args* a, void* ws, size_t ws_bytes, cudaSt
     Carver carve{base_of(ws, ask)};
     Operands op{carve};
     const Mat xo = dw.p ? op(x, a->m, a->k) : x, wo = dx.p ? op(w, a->n, a->k) : w;
-    // dz, as the products read it: dy itself where nothing lies between, the caller's dz, or a matrix of its own
+    // dz, as the products read it: dy itself where nothing lies between, the caller's dz, or a matrix of its own.  16 bits wide, as the tensor
+    // cores take their operands: half a step of each term, which leaves a sum of many terms 1.4 times as far from 64 bits as its own
+    // last rounding does (bf16 2.35e-3 against 1.66e-3, fp16 2.93e-4 against 2.07e-4).  db sums what is not rounded yet.
     const bool products = dx.p || dw.p;
     Mat dz{nullptr, 0};
     if (products) dz = !has_act && dense_rows16(dy) ? dy : dz_out.p && dense_rows16(dz_out) ? dz_out : carve.matrix(a->m, a->n);
@@ -703,6 +707,7 @@ int gated_grad(const dlf_gated_grad_args* a, void* ws, size_t ws_bytes, cudaStre
     Carver carve{base_of(ws, ask)};
     Operands op{carve};
     const Mat xo = any_dw ? op(x, a->m, a->k) : x, wgo = dx.p ? op(wg, a->n, a->k) : wg, wuo = dx.p ? op(wu, a->n, a->k) : wu;
+    // (dg and du are rounded once on their way into the products, as linear_grad's dz is)
     if (dx.p || dwg.p) d.d0 = carve.matrix(a->m, a->n);
     if (dx.p || dwu.p) d.d1 = carve.matrix(a->m, a->n);
     if (only_workspace(ask, carve.used)) return DLF_OK;
